@@ -309,6 +309,122 @@ stx_status stx_rank(stx_ctx *ctx, const stx_params *p, const int32_t *h, const i
                     int64_t nq, int32_t side, float *true_score, int32_t *n_less, int32_t *n_equal, void *work,
                     size_t work_bytes);
 
+/* ---- Rows and products in 8 bits, AdamW ---------------------------------------------------------------
+ *
+ * What a program needs that scores queries against a whole table and trains through it: the query's row as a
+ * normalised sum, the scores as a matrix product of 8-bit operands, the two products of their gradient, and an
+ * optimiser with moments.  These calls take a context for its stream (any model's) and touch nothing else of it
+ * unless they say so.  Element types of rows: */
+enum { STX_F32 = 0, STX_BF16 = 1, STX_F16 = 2 };
+/* Formats of 8-bit codes (OCP): largest numbers 448 and 57344. */
+enum { STX_E4M3 = 0, STX_E5M2 = 1 };
+
+/* A matrix held in 8 bits: codes, and a power of two for each block of 128 columns of each row.  Element (i, j) stands
+ * for code(i, j) * 2^(scales[i * ld_scale + j / 128] - 127).  codes: 16-byte aligned, ld bytes between rows, a multiple
+ * of 16 and at least cols rounded up to 128; the codes from cols up to that are 0 (every call that writes a matrix
+ * writes them).  scales: 4-byte aligned, ld_scale a multiple of 4 and at least the number of blocks; bytes behind the
+ * last block are never used, and not written; they belong to the matrix all the same, the last row's too.  Scale bytes
+ * are 1 to 254.                                                                                              */
+typedef struct {
+    uint8_t *codes;
+    uint8_t *scales;
+    int64_t rows;
+    int64_t cols;
+    int64_t ld;
+    int64_t ld_scale;
+    int32_t format;    /* STX_E4M3 / STX_E5M2 */
+} stx_q8;
+
+/* Root-mean-square norm of rows with the residual's addition:
+ *   s = x + residual, rounded to the rows' type;  y = s * rstd * weight,  rstd = 1 / sqrt(mean(s^2) + eps)
+ * x, residual (null: none), sum and y have `dtype` and ld elements between rows; weight (null: ones) and rstd are fp32.
+ * sum, y, q, rstd are outputs, each may be null (not all four): s, y rounded to the rows' type, y in 8 bits (rounded
+ * once, from fp32), and what the backward pass needs.  sum may be x or residual.  rows >= 0, 1 <= cols <= 16384, ld >= cols; pointers
+ * aligned to their elements only.  Arithmetic is fp32, the sum over a row in a fixed order.
+ * q (rows x cols): the scale of a block is the smallest power of two, 2^-126 at least, that brings its largest finite
+ * magnitude to at most the format's largest number; 1 where there is none but 0.  Codes are rounded to nearest even;
+ * NaN and, in STX_E4M3, infinities become NaN codes (in STX_E5M2 infinities stay).                             */
+stx_status stx_rmsnorm(stx_ctx *ctx, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const void *x,
+                       const void *residual, const float *weight, float eps, void *sum, void *y, const stx_q8 *q,
+                       float *rstd);
+
+/* Backward of stx_rmsnorm from its sum and rstd:
+ *   a = dy * weight;  dx = rstd * (a - s * rstd^2 * mean(a s)) + dsum   (the gradient of x and of residual alike)
+ *   dweight = sum over rows of dy * s * rstd                             (fixed order, no atomics)
+ * dsum (null: none): the gradient that reaches s on other ways.  dweight may be null; rows == 0 gives zeros.  dx may be
+ * dy or dsum.  work: stx_rmsnorm_backward_work_bytes(rows, cols) bytes, 256-byte aligned; null where dweight is.   */
+stx_status stx_rmsnorm_backward_work_bytes(const stx_ctx *ctx, int64_t rows, int64_t cols, size_t *bytes /* host, out */);
+stx_status stx_rmsnorm_backward(stx_ctx *ctx, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const void *sum,
+                                const float *weight, const float *rstd, const void *dy, const void *dsum, void *dx,
+                                float *dweight, void *work, size_t work_bytes);
+
+/* Rows in 8 bits, with scales and rounding as stx_rmsnorm's q: q (rows x cols) the matrix, qt (cols x rows) its
+ * transpose, whose blocks lie along the rows of x (the gradient's products sum over the other axis, and need it).
+ * Either may be null, not both; both read x once.  rows >= 0, cols >= 0, both below 2^31.                     */
+stx_status stx_q8_quantize(stx_ctx *ctx, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const void *x,
+                           const stx_q8 *q, const stx_q8 *qt);
+
+/* out (a->rows x b->rows, `dtype`, ldo elements between rows) = A B^T over a->cols == b->cols columns (at least one), on
+ * the matrix cores; sums are fp32, rounded once into out.  The formats of a and b may differ.  ld of both at most 2^24.
+ * For an fp32 out products are whole.  For a 16-bit out the 8-bit instructions sum them in eights and cut off what lies
+ * below 2^-13 of the largest of an eight: far less than the output's own rounding, unless nearly all of a sum cancels.
+ * out shares no memory with the operands.  work: stx_q8_matmul_work_bytes bytes, 256-byte aligned (products of few
+ * tiles and long rows are cut along the rows and joined there, in a fixed order); null where that says 0.      */
+stx_status stx_q8_matmul_work_bytes(const stx_ctx *ctx, int64_t rows_a, int64_t rows_b, int64_t cols,
+                                    size_t *bytes /* host, out */);
+stx_status stx_q8_matmul(stx_ctx *ctx, const stx_q8 *a, const stx_q8 *b, int32_t dtype, void *out, int64_t ldo,
+                         void *work, size_t work_bytes);
+
+/* AdamW, step number t:
+ *   g' = g * grad_scale;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;
+ *   p = p - lr weight_decay p;  p = p - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, every operation rounded once, the numbers that no element changes formed in double.
+ * bits: 32 (m and v are fp32) or 8.  In 8 bits m is held in STX_E4M3 and v in STX_E5M2 codes, with an fp32 scale for
+ * each block of 128 elements: its largest magnitude over the format's largest number, or 0, with codes of 0, where that
+ * magnitude is below 2^-100.  Values are rounded up or down by random bits, so that what a step adds is kept on the
+ * average where it is less than a code's step; a v above 0 keeps at least the smallest code.  The bits of element i of
+ * tensor n are halves of output number i / 2 of the SplitMix64 sequence seeded with output number t 2^16 + n of the one
+ * seeded with `seed`: element i even takes the low 32 of the 64 bits, m the lower 16 of those.  A block that holds an
+ * infinity or NaN becomes NaN as a whole.  Moments start as zeros (codes and scales).                          */
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;             /* t, from 1 on */
+    const int64_t *step_dev;  /* device, may be null: t is read there instead (below 1 counts as 1), for captured calls */
+    const float *grad_scale;  /* device, may be null (1): one factor for all gradients */
+    uint64_t seed;            /* 8 bits: see above */
+    int32_t bits;             /* 32 / 8 */
+} stx_adamw;
+
+typedef struct {
+    void *m, *v;              /* 32 bits: fp32; 8 bits: one byte an element */
+    float *m_scale, *v_scale; /* 8 bits only: one for each block */
+} stx_moments;
+
+#define STX_ADAMW_NO_DECAY 1u /* stx_adamw_tensor.flags: no weight decay on this tensor */
+typedef struct {
+    float *p;
+    const void *g;
+    int64_t n;                /* elements, contiguous; blocks of 128 from the first on */
+    stx_moments s;
+    int32_t g_dtype;          /* STX_F32 / STX_BF16 / STX_F16 */
+    uint32_t flags;
+} stx_adamw_tensor;
+
+/* One step over n_tensors (at most 65,535) tensors (host array, read before the call returns): one launch for every
+ * 48 of them.  Pointers aligned to their elements.  No two share memory.                                   */
+stx_status stx_adamw_tensors(stx_ctx *ctx, const stx_adamw *h, const stx_adamw_tensor *tensors, int32_t n_tensors);
+
+/* The same step on the touched rows of a batch, in place of stx_sgd_step: rows without a gradient keep p, m and v, and
+ * are not decayed.  TorusE's fractional parts and STX_FLAG_RENORM_W as there.  One set of moments for each table that the
+ * model has, laid out as the table; in 8 bits each row's blocks of 128 begin with the row (the last may be short): codes
+ * as the table's elements, ceil(width / 128) scales for each row; TransR's matrices count as rows of rel_dim * dim.  For
+ * the random bits the tables ent, rel, w, proj are tensors 0 to 3 and elements are counted through the table.  */
+typedef struct {
+    stx_moments ent, rel, w, proj;
+} stx_adamw_state;
+stx_status stx_adamw_step(stx_ctx *ctx, stx_params *p, const stx_incidence *inc, const stx_grads *g, const stx_adamw *h,
+                          const stx_adamw_state *s);
+
 const char *stx_status_string(stx_status s);
 
 #ifdef __cplusplus

@@ -23,12 +23,17 @@ STX_SUM, STX_MEAN = 0, 1
 STX_FLAG_RENORM_W, STX_FLAG_BF16_PROJ = 1, 2
 STX_DISTMULT, STX_COMPLEX, STX_ROTATE = 0, 1, 2
 STX_TAIL, STX_HEAD = 0, 1
+STX_F32, STX_BF16, STX_F16 = 0, 1, 2
+STX_E4M3, STX_E5M2 = 0, 1
+STX_ADAMW_NO_DECAY = 1
 
 MODELS = {"transe": STX_TRANSE, "transh": STX_TRANSH, "transr": STX_TRANSR, "toruse": STX_TORUSE}
+DTYPES = {torch.float32: STX_F32, torch.bfloat16: STX_BF16, torch.float16: STX_F16}
 DISTS = {"l1": STX_L1, "l2": STX_L2, "torus_l1": STX_TORUS_L1, "torus_l2": STX_TORUS_L2, "l2_sq": STX_L2_SQ}
 
 EXPORTS = ["stx_workspace_bytes", "stx_create", "stx_destroy", "stx_sample_negatives", "stx_build_incidence",
-           "stx_check_indices", "stx_spmm", "stx_spmm_semiring", "stx_spmm_semiring_t", "stx_spmm_semiring_t_static", "stx_rank", "stx_rank_work_bytes", "stx_forward", "stx_backward", "stx_sgd_step", "stx_backward_sgd", "stx_train_step", "stx_profile_kernel",
+           "stx_check_indices", "stx_spmm", "stx_spmm_semiring", "stx_spmm_semiring_t", "stx_spmm_semiring_t_static", "stx_rank", "stx_rank_work_bytes", "stx_rmsnorm", "stx_rmsnorm_backward", "stx_rmsnorm_backward_work_bytes",
+           "stx_q8_quantize", "stx_q8_matmul", "stx_q8_matmul_work_bytes", "stx_adamw_tensors", "stx_adamw_step", "stx_forward", "stx_backward", "stx_sgd_step", "stx_backward_sgd", "stx_train_step", "stx_profile_kernel",
            "stx_profile_every", "stx_profile_read", "stx_profile_dump", "stx_copy_f32", "stx_read_sectors", "stx_status_string"]
 
 
@@ -67,6 +72,30 @@ class stx_batch(C.Structure):
                 ("neg_h", C.c_void_p), ("neg_t", C.c_void_p), ("next", C.c_void_p)]
 
 
+class stx_q8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64),
+                ("ld_scale", C.c_int64), ("format", C.c_int32)]
+
+
+class stx_adamw(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("step", C.c_int64), ("step_dev", C.c_void_p), ("grad_scale", C.c_void_p),
+                ("seed", C.c_uint64), ("bits", C.c_int32)]
+
+
+class stx_moments(C.Structure):
+    _fields_ = [("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class stx_adamw_tensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("n", C.c_int64), ("s", stx_moments), ("g_dtype", C.c_int32),
+                ("flags", C.c_uint32)]
+
+
+class stx_adamw_state(C.Structure):
+    _fields_ = [("ent", stx_moments), ("rel", stx_moments), ("w", stx_moments), ("proj", stx_moments)]
+
+
 _lib = None
 
 
@@ -101,6 +130,15 @@ def lib():
                                        C.c_float]
         L.stx_train_step.argtypes = [vp, C.POINTER(stx_batch), C.POINTER(stx_incidence), C.POINTER(stx_params),
                                      C.POINTER(stx_grads), C.c_float, vp, vp]
+        L.stx_rmsnorm.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, C.c_float, vp, vp, C.POINTER(stx_q8), vp]
+        L.stx_rmsnorm_backward_work_bytes.argtypes = [vp, i64, i64, C.POINTER(C.c_size_t)]
+        L.stx_rmsnorm_backward.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t]
+        L.stx_q8_quantize.argtypes = [vp, i32, i64, i64, i64, vp, C.POINTER(stx_q8), C.POINTER(stx_q8)]
+        L.stx_q8_matmul_work_bytes.argtypes = [vp, i64, i64, i64, C.POINTER(C.c_size_t)]
+        L.stx_q8_matmul.argtypes = [vp, C.POINTER(stx_q8), C.POINTER(stx_q8), i32, vp, i64, vp, C.c_size_t]
+        L.stx_adamw_tensors.argtypes = [vp, C.POINTER(stx_adamw), C.POINTER(stx_adamw_tensor), i32]
+        L.stx_adamw_step.argtypes = [vp, C.POINTER(stx_params), C.POINTER(stx_incidence), C.POINTER(stx_grads),
+                                     C.POINTER(stx_adamw), C.POINTER(stx_adamw_state)]
         L.stx_profile_kernel.argtypes = [vp, C.c_char_p, i32]
         L.stx_profile_every.argtypes = [vp, i32]
         L.stx_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(i32)]
@@ -147,6 +185,7 @@ class Context:
     def __init__(self, cfg: stx_config, device="cuda:0", stream: torch.cuda.Stream | None = None):
         self.cfg = cfg
         self.device = torch.device(device)
+        self.index = torch.cuda.current_device() if self.device.index is None else self.device.index
         nbytes = stx_workspace_bytes(cfg)
         self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         base = self.workspace.data_ptr()
@@ -354,6 +393,173 @@ def stx_train_step(ctx: Context, batch, inc: Incidence, p: Params, g, lr: float,
     gp = C.byref(g.c) if g is not None else None
     _check("stx_train_step", lib().stx_train_step(ctx.handle, C.byref(batch), C.byref(inc.c), C.byref(p.c), gp, lr,
                                                   scores.data_ptr(), loss.data_ptr()))
+
+
+class Q8:
+    """A matrix in 8 bits: `codes` (rows x cols rounded up to 128) and `scales` (rows x blocks rounded up to 4), uint8."""
+
+    def __init__(self, rows, cols, format=STX_E4M3, device="cuda:0"):
+        blocks = (cols + 127) // 128
+        self._set(torch.zeros(rows, blocks * 128, dtype=torch.uint8, device=device),
+                  torch.full((rows, (blocks + 3) // 4 * 4), 127, dtype=torch.uint8, device=device), cols, format)
+
+    @classmethod
+    def of(cls, codes, scales, cols, format=STX_E4M3):
+        """Around tensors that a program holds already; the codes behind the last column are 0."""
+        q = cls.__new__(cls)
+        q._set(codes, scales, cols, format)
+        return q
+
+    def _set(self, codes, scales, cols, format):
+        for t in (codes, scales):
+            assert t.is_cuda and t.dtype == torch.uint8 and t.dim() == 2 and t.stride(1) == 1 and t.shape[0] == codes.shape[0]
+        assert codes.shape[1] >= (cols + 127) // 128 * 128 and scales.shape[1] >= (cols + 127) // 128
+        self.codes, self.scales, self.rows, self.cols, self.format = codes, scales, codes.shape[0], cols, format
+        self.c = stx_q8(_ptr(codes), _ptr(scales), codes.shape[0], cols, codes.stride(0), scales.stride(0), format)
+
+
+def _rows2d(ctx, *tensors):
+    """(dtype, rows, cols, ld) of matrices of one type, shape and row stride on the context's device."""
+    first = tensors[0]
+    for t in tensors:
+        assert t is None or (t.get_device() == ctx.index and t.dtype == first.dtype and t.dim() == 2 and t.shape == first.shape and
+                             (t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) == first.stride(0)))
+    rows, cols = first.shape
+    ld = next((t.stride(0) for t in tensors if t is not None and t.shape[0] > 1), cols)
+    return DTYPES[first.dtype], rows, cols, ld
+
+
+def _f32dev(ctx, t, n):
+    assert t is None or (t.get_device() == ctx.index and t.dtype == torch.float32 and t.is_contiguous() and t.numel() >= n)
+    return _ptr(t)
+
+
+def _work(ctx, work):
+    """(pointer, bytes) of the aligned part of a uint8 scratch tensor."""
+    if work is None:
+        return None, 0
+    assert work.get_device() == ctx.index and work.dtype == torch.uint8 and work.is_contiguous()
+    wp = (work.data_ptr() + 255) // 256 * 256
+    return wp, max(0, work.numel() - (wp - work.data_ptr()))
+
+
+def _q8(ctx, q):
+    assert q is None or q.codes.get_device() == q.scales.get_device() == ctx.index
+    return None if q is None else C.byref(q.c)
+
+
+def stx_rmsnorm(ctx: Context, x, residual, weight, eps: float, sum, y, q, rstd):
+    """Rows are matrices of one type, shape and row stride; sum, y, q (Q8) and rstd may be None, as may residual and weight."""
+    dtype, rows, cols, ld = _rows2d(ctx, x, residual, sum, y)
+    _check("stx_rmsnorm", lib().stx_rmsnorm(ctx.handle, dtype, rows, cols, ld, _ptr(x), _ptr(residual), _f32dev(ctx, weight, cols),
+                                            eps, _ptr(sum), _ptr(y), _q8(ctx, q), _f32dev(ctx, rstd, rows)))
+
+
+def stx_rmsnorm_backward_work_bytes(ctx: Context, rows: int, cols: int) -> int:
+    n = C.c_size_t(0)
+    _check("stx_rmsnorm_backward_work_bytes", lib().stx_rmsnorm_backward_work_bytes(ctx.handle, rows, cols, C.byref(n)))
+    return n.value
+
+
+def stx_rmsnorm_backward(ctx: Context, sum, weight, rstd, dy, dsum, dx, dweight, work=None):
+    """work: a uint8 device tensor of at least stx_rmsnorm_backward_work_bytes(rows, cols) + 256 bytes, or None without dweight."""
+    dtype, rows, cols, ld = _rows2d(ctx, sum, dy, dsum, dx)
+    wp, wb = _work(ctx, work)
+    _check("stx_rmsnorm_backward",
+           lib().stx_rmsnorm_backward(ctx.handle, dtype, rows, cols, ld, _ptr(sum), _f32dev(ctx, weight, cols), _f32dev(ctx, rstd, rows),
+                                      _ptr(dy), _ptr(dsum), _ptr(dx), _f32dev(ctx, dweight, cols), wp, wb))
+
+
+def stx_q8_quantize(ctx: Context, x, q, qt):
+    """q (rows x cols) and / or qt (cols x rows) from a matrix; one of them may be None."""
+    dtype, rows, cols, ld = _rows2d(ctx, x)
+    _check("stx_q8_quantize", lib().stx_q8_quantize(ctx.handle, dtype, rows, cols, ld, _ptr(x), _q8(ctx, q), _q8(ctx, qt)))
+
+
+def stx_q8_matmul_work_bytes(ctx: Context, rows_a: int, rows_b: int, cols: int) -> int:
+    n = C.c_size_t(0)
+    _check("stx_q8_matmul_work_bytes", lib().stx_q8_matmul_work_bytes(ctx.handle, rows_a, rows_b, cols, C.byref(n)))
+    return n.value
+
+
+def stx_q8_matmul(ctx: Context, a: Q8, b: Q8, out, work=None):
+    """out = A B^T.  work: a uint8 device tensor of at least stx_q8_matmul_work_bytes(...) + 256 bytes, or None where that is 0."""
+    dtype, rows, cols, ldo = _rows2d(ctx, out)
+    assert (rows, cols) == (a.rows, b.rows)
+    wp, wb = _work(ctx, work)
+    _check("stx_q8_matmul", lib().stx_q8_matmul(ctx.handle, _q8(ctx, a), _q8(ctx, b), dtype, _ptr(out), ldo, wp, wb))
+
+
+def make_adamw(lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, bits=32, step=1, seed=0, step_dev=None,
+               grad_scale=None) -> stx_adamw:
+    """Hyperparameters; a program sets .step before every call.  step_dev (int64) and grad_scale (float32) are device tensors
+    that must stay alive while it is in use."""
+    assert step_dev is None or (step_dev.is_cuda and step_dev.dtype == torch.int64)
+    assert grad_scale is None or (grad_scale.is_cuda and grad_scale.dtype == torch.float32)
+    return stx_adamw(lr, beta1, beta2, eps, weight_decay, step, _ptr(step_dev), _ptr(grad_scale), seed, bits)
+
+
+class _Moments:
+    """m and v of one tensor (float32, or uint8 codes with float32 scales)."""
+
+    def __init__(self, m, v, m_scale=None, v_scale=None):
+        self.bits, self.n, self.blocks = 32 if m_scale is None else 8, m.numel(), 0 if m_scale is None else m_scale.numel()
+        self.index, self.keep = m.get_device(), (m, v, m_scale, v_scale)
+        for t in (m, v):
+            assert t.is_cuda and t.dtype == (torch.float32 if self.bits == 32 else torch.uint8) and t.numel() == self.n
+        for t in (m_scale, v_scale):
+            assert (t is None) == (self.bits == 32)
+            assert t is None or (t.dtype == torch.float32 and t.numel() == self.blocks)
+        assert all(t is None or (t.is_contiguous() and t.get_device() == self.index) for t in self.keep)
+        self.c = stx_moments(*(_ptr(t) for t in self.keep))
+
+
+class AdamWTensors:
+    """The tensors of stx_adamw_tensors: (p, g, m, v[, m_scale, v_scale]) each; m and v are float32, or uint8 codes with a float32
+    scale for each 128 elements.  no_decay: positions of tensors without weight decay."""
+
+    def __init__(self, tensors, no_decay=()):
+        self.keep, self.n = [], len(tensors)
+        self.c = (stx_adamw_tensor * max(1, self.n))()
+        for i, (p, g, *s) in enumerate(tensors):
+            s = _Moments(*s)
+            assert p.is_cuda and p.dtype == torch.float32 and p.is_contiguous() and p.numel() == g.numel() == s.n
+            assert g.is_contiguous() and p.get_device() == g.get_device() == s.index
+            assert s.bits == 32 or s.blocks == (s.n + 127) // 128
+            self.c[i] = stx_adamw_tensor(_ptr(p), _ptr(g), s.n, s.c, DTYPES[g.dtype], STX_ADAMW_NO_DECAY if i in no_decay else 0)
+            self.keep.append((p, g, s))
+        self.places = {(s.index, s.bits) for _, _, s in self.keep}
+
+
+class AdamWState:
+    """Moments of the tables that a model has, (m, v[, m_scale, v_scale]) each, laid out as the tables."""
+
+    def __init__(self, ent, rel=None, w=None, proj=None):
+        self.held = {name: _Moments(*t) for name, t in (("ent", ent), ("rel", rel), ("w", w), ("proj", proj)) if t is not None}
+        self.c = stx_adamw_state(**{name: s.c for name, s in self.held.items()})
+
+    @classmethod
+    def zeros(cls, p: Params, bits=32):
+        def one(t):
+            if t is None:
+                return None
+            like = lambda: torch.zeros(t.shape, dtype=torch.float32 if bits == 32 else torch.uint8, device=t.device)  # noqa: E731
+            scale = lambda: torch.zeros(t.shape[0], (t[0].numel() + 127) // 128, device=t.device)  # noqa: E731
+            return (like(), like()) if bits == 32 else (like(), like(), scale(), scale())
+        return cls(one(p.ent), one(p.rel), one(p.w), one(p.proj))
+
+
+def stx_adamw_tensors(ctx: Context, h: stx_adamw, tensors: AdamWTensors):
+    assert tensors.n == 0 or tensors.places == {(ctx.index, h.bits)}
+    _check("stx_adamw_tensors", lib().stx_adamw_tensors(ctx.handle, C.byref(h), tensors.c, tensors.n))
+
+
+def stx_adamw_step(ctx: Context, p: Params, inc: Incidence, g: Grads, h: stx_adamw, s: AdamWState):
+    for name, m in s.held.items():
+        t = getattr(p, name)
+        assert t is None or (m.n == t.numel() and (m.index, m.bits) == (ctx.index, h.bits) and
+                             (m.bits == 32 or m.blocks == t.shape[0] * ((m.n // t.shape[0] + 127) // 128)))
+    _check("stx_adamw_step", lib().stx_adamw_step(ctx.handle, C.byref(p.c), C.byref(inc.c), C.byref(g.c), C.byref(h), C.byref(s.c)))
 
 
 def stx_profile_kernel(ctx: Context, kernel_name, max_records: int):

@@ -161,6 +161,18 @@ stx_status check_a_current(const stx_ctx *ctx, const stx_incidence *inc)
 
 }  // namespace
 
+// What an update of the touched rows needs (stx_adamw_step).
+stx_status stx::check_update(const stx_ctx *ctx, const stx_params *p, const stx_incidence *inc, const stx_grads *g)
+{
+    stx_status s = check_built(ctx, inc);
+    if (s == STX_OK) s = check_params(ctx, p);
+    if (s != STX_OK) return s;
+    if (!g || !g->rows) return STX_ERR_NULL;
+    if (ctx->cfg.model == STX_TRANSH && !g->w_rows) return STX_ERR_NULL;
+    if (ctx->cfg.model == STX_TRANSR && !g->proj) return STX_ERR_NULL;
+    return STX_OK;
+}
+
 extern "C" {
 
 stx_status stx_workspace_bytes(const stx_config *cfg, size_t *bytes)

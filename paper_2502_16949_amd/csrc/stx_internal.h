@@ -472,6 +472,9 @@ inline FormedRows formed_buffers(const stx_ctx *c, int64_t n_rows)
     return {(float *)b, b + o1, b + o2, (float *)(b + o3), (float *)(b + o1)};
 }
 
+// stx_api.cpp
+stx_status check_update(const stx_ctx *, const stx_params *, const stx_incidence *, const stx_grads *);
+
 inline stx_status hip_ok(hipError_t e) { return e == hipSuccess ? STX_OK : STX_ERR_HIP; }
 
 // Brackets the launches of the kernel selected with stx_profile_kernel by a pair of events on the

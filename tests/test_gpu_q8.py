@@ -1,0 +1,200 @@
+"""stx_q8_quantize and stx_q8_matmul against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2502_16949_amd import binding as B
+from tests import gpu_util as G
+from tests import ops_ref as R
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return B.Context(B.make_config("transe", "l2", 100, 5, 32, 64, 1), G.DEV)
+
+
+def matrix(rng, rows, cols, dtype, ld=None, offset=0, spread=1.0):
+    ld = ld or cols
+    room = torch.full((offset + rows * ld + 8,), float("nan"), dtype=dtype, device=G.DEV)
+    t = room[offset:offset + rows * ld].view(rows, ld)[:, :cols]
+    t.copy_(torch.from_numpy(rng.standard_normal((rows, cols)) * np.exp(spread * rng.standard_normal((rows, 1)))))
+    return t
+
+
+def poisoned(rows, cols, fmt):
+    q = B.Q8(rows, cols, fmt, G.DEV)
+    q.codes.fill_(0x7F)
+    q.scales.fill_(200)
+    return q
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 1024), (3, 127), (128, 128), (129, 130), (257, 64), (77, 1001), (400, 383)])
+def test_quantize_both_ways(ctx, rows, cols, dtype):
+    rng = np.random.default_rng(rows + cols)
+    ld, off = (cols + 3, 1) if cols % 2 else (cols, 0)
+    x = matrix(rng, rows, cols, dtype, ld, off, spread=4.0 if dtype != torch.float16 else 1.0)
+    for fmt, fmt_t in ((0, 0), (0, 1), (1, 0), (1, 1)):
+        q, qt, q1, qt1 = poisoned(rows, cols, fmt), poisoned(cols, rows, fmt_t), poisoned(rows, cols, fmt), poisoned(cols, rows, fmt_t)
+        B.stx_q8_quantize(ctx, x, q, qt)
+        B.stx_q8_quantize(ctx, x, q1, None)
+        B.stx_q8_quantize(ctx, x, None, qt1)
+        R.check_q8(q, R.f64(x))
+        R.check_q8(qt, np.ascontiguousarray(R.f64(x).T))
+        for a, b in ((q, q1), (qt, qt1)):
+            assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
+
+
+def test_quantize_exact_ties_and_edges(ctx):
+    # every code's number and every midpoint between neighbours: nearest even
+    for fmt in (0, 1):
+        pos = np.unique(np.abs(R.decode(np.arange(256, dtype=np.uint8), fmt)))
+        pos = pos[np.isfinite(pos)]
+        mids = (pos[1:] + pos[:-1]) / 2
+        v = np.concatenate([pos, mids])
+        x = np.zeros((-(-len(v) // 127), 128), np.float32)
+        x.reshape(-1)[:] = 0
+        for i, c in enumerate(v):
+            x[i // 127, 1 + i % 127] = c if i % 2 else -c
+        x[:, 0] = pos[-1]                                   # the scale is 1
+        q = poisoned(len(x), 128, fmt)
+        B.stx_q8_quantize(ctx, torch.from_numpy(x).to(G.DEV), q, None)
+        want = torch.from_numpy(x).to(R.FORMATS[fmt][0]).double().numpy()
+        assert (q.scales[:, 0] == 127).all() and np.array_equal(R.q8_numbers(q), want)
+
+
+def test_quantize_extremes(ctx):
+    tiny, big, inf, nan = 2.0**-149, 3.4e38, float("inf"), float("nan")
+    x = torch.zeros(7, 128, device=G.DEV)
+    x[1, 3], x[2, :] = tiny, big
+    x[3, 0], x[3, 1] = inf, 1.0
+    x[4, 0], x[4, 1] = nan, -1.0
+    x[5, 0], x[5, 1] = 2.0**-120, -(2.0**-121)
+    x[6, 0] = 448.0 * (1 + 2.0**-23)                        # just beyond: the next power of two
+    for fmt in (0, 1):
+        q, qt = poisoned(7, 128, fmt), poisoned(128, 7, fmt)
+        B.stx_q8_quantize(ctx, x, q, qt)
+        R.check_q8(q, R.f64(x))
+        R.check_q8(qt, np.ascontiguousarray(R.f64(x).T))
+        assert int(q.scales[0, 0]) == 127 and int(q.scales[1, 0]) == 1
+        assert np.isnan(R.q8_numbers(q)[4, 0])
+
+
+def test_quantize_nothing(ctx):
+    for rows, cols in ((0, 5), (5, 0)):
+        x = torch.empty(rows, cols, device=G.DEV)
+        q = B.Q8(rows, cols, B.STX_E4M3, G.DEV)
+        B.stx_q8_quantize(ctx, x, q, None)
+
+
+def _q8_of(rng, rows, cols, fmt):
+    """A matrix of random codes (no NaN, no infinity) and scales, in a buffer with room between rows."""
+    nb = -(-cols // 128)
+    codes = rng.integers(0, 256, (rows, nb * 128 + 16), dtype=np.uint8)
+    bad = (codes & 0x7F) >= (0x7F if fmt == 0 else 0x7C)
+    codes[bad] &= 0x3F
+    codes[:, cols:nb * 128] = 0
+    scales = rng.integers(118, 137, (rows, (nb + 3) // 4 * 4 + 4), dtype=np.uint8)
+    scales[:, nb:] = 255                                    # never used
+    codes[:, nb * 128:] = 0x7F
+    q = B.Q8.of(torch.from_numpy(codes).to(G.DEV), torch.from_numpy(scales).to(G.DEV), cols, fmt)
+    return q, R.held(codes, scales, cols, fmt)
+
+
+def run(ctx, a, b, dtype, ldo=None):
+    ldo = ldo or b.rows
+    room = torch.full((a.rows, ldo), 777.0, dtype=dtype, device=G.DEV)
+    need = B.stx_q8_matmul_work_bytes(ctx, a.rows, b.rows, a.cols)
+    work = torch.full((need + 256,), 0x7F, dtype=torch.uint8, device=G.DEV)
+    B.stx_q8_matmul(ctx, a, b, room[:, :b.rows], work)
+    assert (room[:, b.rows:] == 777.0).all()
+    return room[:, :b.rows]
+
+
+def check_product(got, x, y, dtype, cols):
+    """fp32: the sums of each 32 products, at most four groups that are cut below 2^-23 of the running sum and 16 cut-offs within
+    them.  16 bits: in every eight products up to seven are cut below 2^-13 of the eight's largest.  Then one rounding."""
+    want, total = x @ y.T, np.abs(x) @ np.abs(y).T
+    nb = -(-cols // 128)
+    tol = (4 * 4 * nb + 16) * 2.0**-23 * total + 2 * R.HALF[dtype] * np.abs(want) + (2.0**-25 if dtype == torch.float16 else 0)
+    if dtype != torch.float32:
+        tol += 7 * 2.0**-13 * total
+    err = np.abs(R.f64(got) - want)
+    print("%s: share of the bound %.3g, of the sizes' sum %.3g" % (dtype, np.max(err / np.maximum(tol, 1e-300)), np.max(err / total)))
+    assert np.all(err <= tol), (np.argwhere(err > tol)[:5], np.max(err / np.maximum(tol, 1e-300)))
+
+
+SIZES = [(1, 1, 1), (1, 17, 128), (2, 300, 129), (16, 16, 256), (17, 33, 1000), (5, 1500, 1024), (31, 700, 384), (64, 64, 640), (65, 129, 127),
+         (100, 500, 2048), (128, 256, 512), (129, 257, 513), (255, 511, 896), (300, 1000, 100), (520, 130, 1500), (1, 4000, 8192),
+         (700, 90, 20000), (257, 1030, 4100)]
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_product(ctx, m, n, k):
+    rng = np.random.default_rng(m + n + k)
+    a, x = _q8_of(rng, m, k, 0)
+    b, y = _q8_of(rng, n, k, 0)
+    for dtype, ldo in ((torch.float32, None), (torch.bfloat16, n + 3)):
+        check_product(run(ctx, a, b, dtype, ldo), x, y, dtype, k)
+
+
+@pytest.mark.parametrize("fa,fb", [(0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("m,n,k", [(3, 70, 300), (130, 300, 700), (300, 300, 256)])
+def test_product_formats(ctx, m, n, k, fa, fb):
+    rng = np.random.default_rng(fa * 2 + fb + m)
+    a, x = _q8_of(rng, m, k, fa)
+    b, y = _q8_of(rng, n, k, fb)
+    check_product(run(ctx, a, b, torch.float32), x, y, torch.float32, k)
+
+
+def test_product_fp16_out(ctx):
+    rng = np.random.default_rng(1)
+    xs, ys = (torch.from_numpy(rng.standard_normal((r, 512)).astype(np.float32)).to(G.DEV) for r in (140, 270))
+    a, b = B.Q8(140, 512, 0, G.DEV), B.Q8(270, 512, 0, G.DEV)
+    B.stx_q8_quantize(ctx, xs, a, None)
+    B.stx_q8_quantize(ctx, ys, b, None)
+    check_product(run(ctx, a, b, torch.float16, 275), R.q8_numbers(a), R.q8_numbers(b), torch.float16, 512)
+
+
+def test_product_of_exact_sums(ctx):
+    # small whole numbers: no sum rounds, so every output is exact
+    rng = np.random.default_rng(2)
+    for m, n, k in ((7, 100, 1000), (200, 300, 1024), (600, 520, 384)):
+        xs, ys = (rng.integers(-3, 4, (r, k)).astype(np.float32) for r in (m, n))
+        a, b = B.Q8(m, k, 0, G.DEV), B.Q8(n, k, 0, G.DEV)
+        B.stx_q8_quantize(ctx, torch.from_numpy(xs).to(G.DEV), a, None)
+        B.stx_q8_quantize(ctx, torch.from_numpy(ys).to(G.DEV), b, None)
+        assert np.array_equal(R.f64(run(ctx, a, b, torch.float32)), xs.astype(np.float64) @ ys.T.astype(np.float64))
+
+
+def test_product_with_nan_rows(ctx):
+    # a row that is not finite spoils its own outputs only
+    rng = np.random.default_rng(4)
+    for m, n, k in ((3, 200, 256), (300, 300, 256)):
+        a, x = _q8_of(rng, m, k, 0)
+        b, y = _q8_of(rng, n, k, 0)
+        a.codes[1, 200] = 0x7F
+        b.codes[n - 1, 3] = 0xFF
+        got = R.f64(run(ctx, a, b, torch.float32))
+        bad = np.zeros((m, n), bool)
+        bad[1], bad[:, n - 1] = True, True
+        assert np.isnan(got[bad]).all() and np.isfinite(got[~bad]).all()
+
+
+def test_product_same_bits_again(ctx):
+    rng = np.random.default_rng(5)
+    a, _ = _q8_of(rng, 60, 9000, 0)
+    b, _ = _q8_of(rng, 80, 9000, 0)
+    assert torch.equal(run(ctx, a, b, torch.float32), run(ctx, a, b, torch.float32))
+
+
+def test_product_of_nothing(ctx):
+    b = B.Q8(5, 64, 0, G.DEV)
+    for m, n in ((0, 5), (5, 0)):
+        a, c = (B.Q8(r, 64, 0, G.DEV) for r in (m, n))
+        B.stx_q8_matmul(ctx, a, c, torch.empty(m, n, device=G.DEV))
+    del b

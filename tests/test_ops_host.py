@@ -1,0 +1,208 @@
+"""What the entry points of the operators on rows and tensors refuse, before anything is launched: no GPU needed."""
+import ctypes as C
+
+import pytest
+
+from paper_2502_16949_amd import binding as B
+
+L = B.lib()
+P = 4096                                    # an aligned address that is never read
+
+
+def context(model="transe", dim=32, rel_dim=0, flags=0):
+    """A block that begins with the configuration, as a context does: argument checks read no more of it."""
+    cfg = B.make_config(model, "l2", 100, 5, dim, 64, 1, rel_dim=rel_dim, flags=flags)
+    block = (C.c_char * 65536)()
+    C.memmove(block, C.byref(cfg), C.sizeof(cfg))
+    return block
+
+
+def q8(rows=4, cols=200, codes=P, scales=P, ld=256, ld_scale=4, fmt=0, **kw):
+    return B.stx_q8(codes, scales, rows, cols, ld, ld_scale, fmt)
+
+
+def test_struct_sizes():
+    assert (C.sizeof(B.stx_q8), C.sizeof(B.stx_adamw), C.sizeof(B.stx_moments), C.sizeof(B.stx_adamw_tensor),
+            C.sizeof(B.stx_adamw_state)) == (56, 80, 32, 64, 128)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(), B.STX_OK),                     # no rows: nothing to do
+    (dict(ctx=None), B.STX_ERR_NULL),
+    (dict(dtype=3), B.STX_ERR_BAD_ARG),
+    (dict(rows=-1), B.STX_ERR_BAD_ARG),
+    (dict(rows=1 << 31), B.STX_ERR_BAD_ARG),
+    (dict(cols=0), B.STX_ERR_BAD_ARG),
+    (dict(cols=16385, ld=16385), B.STX_ERR_BAD_ARG),
+    (dict(ld=199), B.STX_ERR_BAD_ARG),
+    (dict(eps=-1e-6), B.STX_ERR_BAD_ARG),
+    (dict(eps=float("nan")), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, x=None), B.STX_ERR_NULL),
+    (dict(rows=4, y=None), B.STX_ERR_NULL),                 # no output at all
+    (dict(rows=4, x=P + 2), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, rstd=P + 2), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, dtype=B.STX_BF16, x=P + 1), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, q=q8(rows=5)), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, q=q8(cols=201)), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, q=q8(fmt=2)), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, q=q8(ld=200)), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, q=q8(ld=264)), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, q=q8(ld_scale=2)), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, q=q8(codes=P + 8)), B.STX_ERR_BAD_ARG),
+    (dict(rows=4, q=q8(scales=None)), B.STX_ERR_NULL),
+])
+def test_rmsnorm_refusals(kw, status):
+    a = dict(ctx=context(), dtype=B.STX_F32, rows=0, cols=200, ld=200, x=P, res=None, w=None, eps=1e-6, sum=None, y=P, q=None, rstd=None)
+    a.update(kw)
+    if isinstance(a["q"], B.stx_q8):
+        a["q"] = C.byref(a["q"])
+    assert L.stx_rmsnorm(*a.values()) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rows=0, dweight=None), B.STX_OK),
+    (dict(dtype=-1), B.STX_ERR_BAD_ARG),
+    (dict(cols=0), B.STX_ERR_BAD_ARG),
+    (dict(ld=100), B.STX_ERR_BAD_ARG),
+    (dict(dy=None), B.STX_ERR_NULL),
+    (dict(rstd=None), B.STX_ERR_NULL),
+    (dict(dx=None), B.STX_ERR_NULL),
+    (dict(dsum=P + 1), B.STX_ERR_BAD_ARG),
+    (dict(work=None), B.STX_ERR_NULL),
+    (dict(work=P + 64), B.STX_ERR_WORKSPACE),
+    (dict(work_bytes=100), B.STX_ERR_WORKSPACE),
+])
+def test_rmsnorm_backward_refusals(kw, status):
+    a = dict(ctx=context(), dtype=B.STX_F32, rows=8, cols=200, ld=200, sum=P, w=P, rstd=P, dy=P, dsum=None, dx=P, dweight=P, work=P,
+             work_bytes=1 << 20)
+    a.update(kw)
+    assert L.stx_rmsnorm_backward(*a.values()) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rows=0, q=q8(rows=0)), B.STX_OK),
+    (dict(q=None), B.STX_ERR_NULL),
+    (dict(dtype=7), B.STX_ERR_BAD_ARG),
+    (dict(cols=-1), B.STX_ERR_BAD_ARG),
+    (dict(ld=10), B.STX_ERR_BAD_ARG),
+    (dict(x=None), B.STX_ERR_NULL),
+    (dict(x=P + 2), B.STX_ERR_BAD_ARG),
+    (dict(q=q8(rows=3)), B.STX_ERR_BAD_ARG),
+    (dict(qt=q8()), B.STX_ERR_BAD_ARG),                     # not the transpose's size
+    (dict(qt=q8(rows=200, cols=4, ld=112)), B.STX_ERR_BAD_ARG),
+    (dict(rows=1 << 30, cols=1 << 20, ld=1 << 20, q=q8(rows=1 << 30, cols=1 << 20, ld=1 << 20, ld_scale=1 << 13)), B.STX_ERR_UNSUPPORTED),
+])
+def test_quantize_refusals(kw, status):
+    a = dict(ctx=context(), dtype=B.STX_F32, rows=4, cols=200, ld=200, x=P, q=q8(), qt=None)
+    a.update(kw)
+    for k in ("q", "qt"):
+        a[k] = None if a[k] is None else C.byref(a[k])
+    assert L.stx_q8_quantize(*a.values()) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(a=q8(rows=0)), B.STX_OK),
+    (dict(b=q8(rows=0)), B.STX_OK),
+    (dict(a=None), B.STX_ERR_NULL),
+    (dict(b=q8(cols=201)), B.STX_ERR_BAD_ARG),
+    (dict(a=q8(cols=0), b=q8(cols=0)), B.STX_ERR_BAD_ARG),
+    (dict(a=q8(rows=-1)), B.STX_ERR_BAD_ARG),
+    (dict(dtype=5), B.STX_ERR_BAD_ARG),
+    (dict(ldo=3), B.STX_ERR_BAD_ARG),
+    (dict(out=None), B.STX_ERR_NULL),
+    (dict(out=P + 2), B.STX_ERR_BAD_ARG),
+    (dict(a=q8(ld=(1 << 24) + 16)), B.STX_ERR_UNSUPPORTED),
+    (dict(a=q8(rows=1 << 30), b=q8(rows=1 << 30), ldo=1 << 30), B.STX_ERR_UNSUPPORTED),
+    (dict(a=q8(cols=100_000, ld=100_096, ld_scale=784), b=q8(cols=100_000, ld=100_096, ld_scale=784), work=None), B.STX_ERR_NULL),
+    (dict(a=q8(cols=100_000, ld=100_096, ld_scale=784), b=q8(cols=100_000, ld=100_096, ld_scale=784), work_bytes=4), B.STX_ERR_WORKSPACE),
+])
+def test_matmul_refusals(kw, status):
+    a = dict(ctx=context(), a=q8(), b=q8(), dtype=B.STX_F32, out=P, ldo=4, work=P, work_bytes=1 << 30)
+    a.update(kw)
+    for k in ("a", "b"):
+        a[k] = None if a[k] is None else C.byref(a[k])
+    assert L.stx_q8_matmul(*a.values()) == status
+
+
+def test_work_sizes():
+    n = C.c_size_t(7)
+    ctx = context()
+    assert L.stx_q8_matmul_work_bytes(ctx, 0, 5, 64, C.byref(n)) == B.STX_OK and n.value == 0
+    assert L.stx_q8_matmul_work_bytes(ctx, 4, 5, 0, C.byref(n)) == B.STX_ERR_BAD_ARG
+    assert L.stx_q8_matmul_work_bytes(ctx, 4, 5, 64, None) == B.STX_ERR_NULL
+    assert L.stx_q8_matmul_work_bytes(None, 4, 5, 64, C.byref(n)) == B.STX_ERR_NULL
+    assert L.stx_rmsnorm_backward_work_bytes(ctx, 1000, 1001, C.byref(n)) == B.STX_OK and n.value % 256 == 0 and n.value >= 4004
+    assert L.stx_rmsnorm_backward_work_bytes(ctx, 1000, 0, C.byref(n)) == B.STX_ERR_BAD_ARG
+
+
+def hyper(**kw):
+    a = dict(lr=0.1, bits=32, step=1)
+    a.update(kw)
+    return B.make_adamw(**a)
+
+
+BAD_HYPER = [dict(bits=16), dict(lr=float("nan")), dict(beta1=1.0), dict(beta2=-0.1), dict(beta2=float("nan")), dict(eps=-1.0), dict(step=0),
+             dict(weight_decay=float("nan"))]
+
+
+@pytest.mark.parametrize("kw", BAD_HYPER)
+def test_adamw_hyperparameters(kw):
+    h = hyper(**kw)
+    assert L.stx_adamw_tensors(context(), C.byref(h), None, 0) == B.STX_ERR_BAD_ARG
+    assert L.stx_adamw_tensors(context(), C.byref(hyper()), None, 0) == B.STX_OK
+
+
+@pytest.mark.parametrize("kw,bits,status", [
+    (dict(n=0, p=None, g=None), 32, B.STX_OK),
+    (dict(n=-1), 32, B.STX_ERR_BAD_ARG),
+    (dict(p=None), 32, B.STX_ERR_NULL),
+    (dict(g=None), 32, B.STX_ERR_NULL),
+    (dict(p=P + 2), 32, B.STX_ERR_BAD_ARG),
+    (dict(g=P + 2), 32, B.STX_ERR_BAD_ARG),
+    (dict(m=None), 32, B.STX_ERR_NULL),
+    (dict(v=P + 1), 32, B.STX_ERR_BAD_ARG),
+    (dict(ms=None), 8, B.STX_ERR_NULL),
+    (dict(vs=P + 2), 8, B.STX_ERR_BAD_ARG),
+    (dict(dtype=9), 32, B.STX_ERR_BAD_ARG),
+    (dict(flags=2), 32, B.STX_ERR_BAD_ARG),
+])
+def test_adamw_tensor_refusals(kw, bits, status):
+    a = dict(p=P, g=P, n=10, m=P, v=P, ms=P, vs=P, dtype=0, flags=0)
+    a.update(kw)
+    t = B.stx_adamw_tensor(a["p"], a["g"], a["n"], B.stx_moments(a["m"], a["v"], a["ms"], a["vs"]), a["dtype"], a["flags"])
+    assert L.stx_adamw_tensors(context(), C.byref(hyper(bits=bits)), C.byref(t), 1) == status
+
+
+def test_adamw_tensor_counts():
+    assert L.stx_adamw_tensors(context(), C.byref(hyper()), None, 1) == B.STX_ERR_NULL
+    assert L.stx_adamw_tensors(context(), C.byref(hyper()), None, 65536) == B.STX_ERR_BAD_ARG
+    assert L.stx_adamw_tensors(None, C.byref(hyper()), None, 0) == B.STX_ERR_NULL
+    assert L.stx_adamw_tensors(context(), None, None, 0) == B.STX_ERR_NULL
+
+
+def _step(ctx, p=None, g=None, h=None, s=None, b=0):
+    inc = B.stx_incidence(b, 1, b * 2, b * 6, *([P] * 10))
+    return L.stx_adamw_step(ctx, C.byref(p or B.stx_params(P, P, P, P, None)), C.byref(inc), C.byref(g or B.stx_grads(P, P, P)),
+                            C.byref(h or hyper()), C.byref(s or B.stx_adamw_state(*([B.stx_moments(P, P, P, P)] * 4))))
+
+
+def test_adamw_step_refusals():
+    bf16 = B.STX_FLAG_BF16_PROJ
+    m = B.stx_moments(P, P, P, P)
+    none = B.stx_moments()
+    assert _step(context()) == B.STX_OK                     # a batch of nothing
+    assert _step(context(), p=B.stx_params()) == B.STX_ERR_NULL
+    assert _step(context(), g=B.stx_grads()) == B.STX_ERR_NULL
+    assert _step(context(), b=65) == B.STX_ERR_BAD_ARG
+    assert _step(context(), h=hyper(bits=4)) == B.STX_ERR_BAD_ARG
+    assert _step(context(), s=B.stx_adamw_state(none, m, m, m)) == B.STX_ERR_NULL
+    assert _step(context(), s=B.stx_adamw_state(m, none, none, none)) == B.STX_OK
+    assert _step(context("transh"), s=B.stx_adamw_state(m, none, m, none)) == B.STX_ERR_NULL
+    assert _step(context("transh"), s=B.stx_adamw_state(m, m, none, none)) == B.STX_ERR_NULL
+    assert _step(context("transh"), g=B.stx_grads(P, None, None)) == B.STX_ERR_NULL
+    assert _step(context("transr", 32, 32, bf16), s=B.stx_adamw_state(m, m, none, none)) == B.STX_ERR_NULL
+    assert _step(context("transr", 32, 32, bf16), g=B.stx_grads(P, None, None)) == B.STX_ERR_NULL
+    assert _step(context(), s=B.stx_adamw_state(B.stx_moments(P + 4, P), m, m, m)) == B.STX_ERR_BAD_ARG        # rows are read in float4
+    assert _step(context(), h=hyper(bits=8), s=B.stx_adamw_state(B.stx_moments(P + 2, P, P, P), m, m, m)) == B.STX_ERR_BAD_ARG
+    assert _step(context(), h=hyper(bits=8), s=B.stx_adamw_state(B.stx_moments(P, P), m, m, m)) == B.STX_ERR_NULL
+    assert L.stx_adamw_step(None, None, None, None, None, None) == B.STX_ERR_NULL
