@@ -117,7 +117,7 @@ __device__ inline void encode(const float (&x)[4 * NQ], uint32_t most, const uin
     const float big = __builtin_bit_cast(float, most);
     const bool live = most >= 0x0d800000u;                                      // 2^-100
     scale = live ? (most < kInfBits ? big * (1.0f / TOP) : __builtin_bit_cast(float, 0x7fc00000u)) : 0.f;
-    const float up = TOP / big;
+    const float up = (1.0f / big) * TOP;
     float y[4 * NQ];
 #pragma unroll
     for (int j = 0; j < 4 * NQ; ++j) {
