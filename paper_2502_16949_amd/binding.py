@@ -418,14 +418,16 @@ class Q8:
         self.c = stx_q8(_ptr(codes), _ptr(scales), codes.shape[0], cols, codes.stride(0), scales.stride(0), format)
 
 
-def _rows2d(ctx, *tensors):
-    """(dtype, rows, cols, ld) of matrices of one type, shape and row stride on the context's device."""
-    first = tensors[0]
-    for t in tensors:
-        assert t is None or (t.get_device() == ctx.index and t.dtype == first.dtype and t.dim() == 2 and t.shape == first.shape and
-                             (t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) == first.stride(0)))
-    rows, cols = first.shape
-    ld = next((t.stride(0) for t in tensors if t is not None and t.shape[0] > 1), cols)
+def _rows2d(ctx, first, *others):
+    """(dtype, rows, cols, ld) of matrices of one type, shape and row stride on the context's device; others may be None."""
+    (rows, cols), stride = first.shape, first.stride()
+    assert first.get_device() == ctx.index and (stride[1] == 1 or cols == 1)
+    ld = stride[0] if rows > 1 else cols
+    for t in others:
+        if t is not None:
+            assert t.dtype is first.dtype and t.shape == first.shape and t.get_device() == ctx.index
+            s = t.stride()
+            assert s == stride or ((s[1] == 1 or cols == 1) and (s[0] == ld or rows <= 1))
     return DTYPES[first.dtype], rows, cols, ld
 
 

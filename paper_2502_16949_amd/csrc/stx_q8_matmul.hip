@@ -35,8 +35,8 @@ struct MmArgs {
     int dtype;
 };
 
-// One fragment of an operand: 32 codes a lane, row lane % 16, columns 32 (lane / 16) on.  Which column a lane holds does not
-// matter to a sum as long as both operands agree.
+// One fragment of an operand: 32 codes a lane, of row lane % 16.  Which columns a lane holds does not matter to a sum as long as
+// both operands agree.
 template <int FORMAT>
 __device__ inline bf16x2_t widen2(int w, float scale, bool hi)
 {
@@ -140,8 +140,8 @@ typedef const __attribute__((address_space(1))) void *global_ptr_t;
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
 
 // A BM x BN tile by WM x WN wavefronts.  A step is one block of 128 columns: its codes go straight to LDS, a row's 128 bytes
-// in a line whose 16-byte pieces are permuted by the row (piece c of row r at c ^ (r % 8)), so that 16 lanes that read the same
-// piece of 16 rows meet every bank once a turn.  Two buffers: a step's loads are under way while the one before it is computed.
+// in a line whose 16-byte pieces are permuted by the row (piece c of row r at c ^ (r / 2 % 8)), and a lane reads
+// pieces g and g + 4 of its row, g = lane / 16: 2.88 ns a read and CU, as 64 lanes side by side; pieces 2 g and 2 g + 1 3.65.  Two buffers: a step's loads are under way while the one before it is computed.
 template <int BM, int BN, int WM, int WN, bool WIDE, int FA, int FB>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
 {
@@ -156,7 +156,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int kb0 = split * p.kb_split, kb1 = min(kb0 + p.kb_split, p.nkb);
     // loads: a wavefront's 64 pieces are 8 rows; rows behind the last one repeat it
-    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    static_assert(NW % 2 == 0, "a wavefront's rows begin at the same place of 16 in every round");
+    const int piece = ((lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7)) * 16;
     uint32_t oa[LA], ob[LB];
 #pragma unroll
     for (int i = 0; i < LA; ++i) oa[i] = (uint32_t)(min((int64_t)((i * NW + wave) * 8 + (lane >> 3)), p.m - 1 - m0) * p.lda) + piece;
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    const int at0 = l15 * kBlock + ((2 * kg) ^ (l15 & 7)) * 16, at1 = l15 * kBlock + ((2 * kg + 1) ^ (l15 & 7)) * 16;
+    const int at0 = l15 * kBlock + (kg ^ (l15 >> 1)) * 16, at1 = l15 * kBlock + ((kg + 4) ^ (l15 >> 1)) * 16;
     auto compute = [&](const uint8_t *sa, const uint8_t *sb, int kb) {
         const uint8_t *sc = reinterpret_cast<const uint8_t *>(s_scale[(kb >> 2) & 1]) + (kb & 3);
         uint32_t scb[NI], sca[MI];
@@ -263,16 +264,112 @@ __global__ __launch_bounds__(kThreads) void k_q8_join(const float *__restrict__ 
     store4(p, 0, i, j, t);
 }
 
-// What a product is cut into.
+// Products of few rows on one side: every row of the other is read once, and that bounds them.  A wavefront multiplies MI x NI
+// tiles of 16 x 16 straight from memory, widened whatever the output (the matrix cores wait here).  KS wavefronts share a tile,
+// each with every KS-th block of columns, and join their sums in order through LDS, so that a short table still has enough
+// loads under way.
+template <int MI, int NI, int KS, int FA, int FB>
+__global__ __launch_bounds__(kThreads) void k_q8_direct(MmArgs p)
+{
+    constexpr int NW = kThreads / 64;
+    __shared__ __align__(16) float s_part[KS > 1 ? NW * MI * NI * 256 : 4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, kg = lane >> 4, ks = wave % KS;
+    const int64_t tile = (int64_t)blockIdx.x * (NW / KS) + wave / KS;
+    const int64_t tm = tile % p.ntm, tn = tile / p.ntm;
+    const bool in = tn < p.ntn;            // (KS > 1: a workgroup's wavefronts alike, as the grid is exact)
+    f32x4_t acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if (in) {
+        const uint8_t *ra[MI], *sa[MI], *rb[NI], *sb[NI];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int64_t r = min((tm * MI + i) * 16 + l15, p.m - 1);
+            ra[i] = p.a + r * p.lda;
+            sa[i] = p.as + r * p.ldas;
+        }
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int64_t r = min((tn * NI + j) * 16 + l15, p.n - 1);
+            rb[j] = p.b + r * p.ldb;
+            sb[j] = p.bs + r * p.ldbs;
+        }
+        for (int kb = ks; kb < p.nkb; kb += KS) {
+            const int at0 = kb * kBlock + kg * 16, at1 = at0 + 64;
+            Piece<false> qa[MI], qb[NI];
+            uint32_t ba[MI], bb[NI];
+#pragma unroll
+            for (int j = 0; j < NI; ++j) { qb[j].load(rb[j], at0, at1, 0); bb[j] = sb[j][kb]; }
+#pragma unroll
+            for (int i = 0; i < MI; ++i) { qa[i].load(ra[i], at0, at1, 0); ba[i] = sa[i][kb]; }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                Frag<true, FB> fb[NI];
+#pragma unroll
+                for (int j = 0; j < NI; ++j) fb[j].set(Piece<true>{half ? qb[j].hi : qb[j].lo}, bb[j]);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    Frag<true, FA> fa;
+                    fa.set(Piece<true>{half ? qa[i].hi : qa[i].lo}, ba[i]);
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] = multiply<FA, FB>(fb[j], fa, acc[i][j]);
+                }
+            }
+        }
+    }
+    if constexpr (KS > 1) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) *reinterpret_cast<f32x4_t *>(s_part + ((wave * MI * NI + i * NI + j) * 64 + lane) * 4) = acc[i][j];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < MI * NI; ++u) {                  // a wavefront joins every KS-th tile
+            if (u % KS != ks) continue;
+            f32x4_t t = *reinterpret_cast<const f32x4_t *>(s_part + (((wave - ks) * MI * NI + u) * 64 + lane) * 4);
+#pragma unroll
+            for (int w = 1; w < KS; ++w) t += *reinterpret_cast<const f32x4_t *>(s_part + (((wave - ks + w) * MI * NI + u) * 64 + lane) * 4);
+            store4(p, 0, (tm * MI + u / NI) * 16 + l15, (tn * NI + u % NI) * 16 + kg * 4, t);
+        }
+    } else if (in) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) store4(p, 0, (tm * MI + i) * 16 + l15, (tn * NI + j) * 16 + kg * 4, acc[i][j]);
+    }
+}
+
+// What a product is cut into: tiles of bm x bn in `splits` slices of the columns, or, for `direct`, tiles of 16 mi x 16 ni whose
+// columns `ks` wavefronts share.
 struct MmPlan {
-    int bm, bn;
+    bool direct;
+    int bm, bn, mi, ni, ks;
     int64_t ntm, ntn;
     int splits, kb_split;
 };
 static MmPlan mm_plan(int64_t m, int64_t n, int64_t k)
 {
     MmPlan t{};
-    const int64_t nkb = (k + kBlock - 1) / kBlock;
+    const int64_t nkb = (k + kBlock - 1) / kBlock, few = m < n ? m : n;
+    t.splits = 1;
+    t.kb_split = (int)nkb;
+    // Tiles of 16 x 16 for tables of up to 4,096 rows, where a workgroup for every 32 would leave compute units idle (16 rows by
+    // 300 over 1,024 columns 3.0 us, in 16 x 32 3.5); 16 x 32 above (by 40,000 rows 10.6 us against 12.9).  From 2^18 rows on
+    // there are loads enough without sharing the columns, and tiles of 16 x 64 (16 by 4 M over 128 columns 146 us, in shared 16 x 32
+    // 179; by 40,000 over 1,024 13.2 against 10.6).  17 to 32 rows: 2 x 2 tiles (32 by 40,000 over 1,024 13.4 us, in 128 x 128 17.8).
+    if (few <= 32) {
+        const int64_t many = m < n ? n : m;
+        const int across = few > 16 ? 2 : many >= ((int64_t)1 << 18) ? 4 : many > 4096 ? 2 : 1;
+        t.direct = true;
+        t.mi = few > 16 ? 2 : m > n ? across : 1;
+        t.ni = few > 16 ? 2 : m > n ? 1 : across;
+        t.ks = many >= ((int64_t)1 << 18) ? 1 : 4;
+        t.ntm = (m + 16 * t.mi - 1) / (16 * t.mi);
+        t.ntn = (n + 16 * t.ni - 1) / (16 * t.ni);
+        return t;
+    }
     const int64_t big = ((m + 255) / 256) * ((n + 255) / 256);
     t.bm = t.bn = big >= 192 ? 256 : 128;
     t.ntm = (m + t.bm - 1) / t.bm;
@@ -297,6 +394,21 @@ size_t q8_matmul_work_bytes(int64_t m, int64_t n, int64_t k)
 template <int FA, int FB>
 static void mm_go(stx_ctx *c, const MmPlan &t, bool wide, const MmArgs &p)
 {
+    if (t.direct) {
+        const int per = 4 / t.ks;
+        const dim3 grid((unsigned)((t.ntm * t.ntn + per - 1) / per));
+        ProfScope prof(c, "k_q8_direct");
+#define STX_DIRECT(MI, NI, KS) hipLaunchKernelGGL((k_q8_direct<MI, NI, KS, FA, FB>), grid, dim3(256), 0, c->stream, p)
+        if (t.mi == 2 && t.ni == 2 && t.ks == 4) STX_DIRECT(2, 2, 4);
+        else if (t.mi == 2 && t.ni == 2) STX_DIRECT(2, 2, 1);
+        else if (t.mi == 4) STX_DIRECT(4, 1, 1);
+        else if (t.ni == 4) STX_DIRECT(1, 4, 1);
+        else if (t.mi == 2) STX_DIRECT(2, 1, 4);
+        else if (t.ni == 2) STX_DIRECT(1, 2, 4);
+        else STX_DIRECT(1, 1, 4);
+#undef STX_DIRECT
+        return;
+    }
     const dim3 grid((unsigned)(t.ntm * t.ntn * t.splits));
     ProfScope prof(c, "k_q8_mm");
     if (t.bm == 256) {
