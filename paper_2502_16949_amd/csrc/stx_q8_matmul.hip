@@ -33,6 +33,7 @@ struct MmArgs {
     void *out;                             // splits > 1: fp32 [split][m][n] instead, with ldo = n
     int64_t ldo;
     int dtype;
+    int past;                              // rows of out are whole lines
 };
 
 // One fragment of an operand: 32 codes a lane, of row lane % 16.  Which columns a lane holds does not matter to a sum as long as
@@ -139,24 +140,202 @@ __device__ inline void tile_of(const MmArgs &p, int &tm, int &tn, int &split)
 typedef const __attribute__((address_space(1))) void *global_ptr_t;
 typedef __attribute__((address_space(3))) void *lds_ptr_t;
 
-// A BM x BN tile by WM x WN wavefronts.  A step is one block of 128 columns: its codes go straight to LDS, a row's 128 bytes
-// in a line whose 16-byte pieces are permuted by the row (piece c of row r at c ^ (r / 2 % 8)), and a lane reads
-// pieces g and g + 4 of its row, g = lane / 16: 2.88 ns a read and CU, as 64 lanes side by side; pieces 2 g and 2 g + 1 3.65.  Two buffers: a step's loads are under way while the one before it is computed.
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+template <int FA, int FB>
+__device__ inline f32x16_t multiply32(const i32x4_t *b, uint32_t scale_b, const i32x4_t *a, uint32_t scale_a, f32x16_t acc)
+{
+    const i32x8_t av = {a[0][0], a[0][1], a[0][2], a[0][3], a[1][0], a[1][1], a[1][2], a[1][3]};
+    const i32x8_t bv = {b[0][0], b[0][1], b[0][2], b[0][3], b[1][0], b[1][1], b[1][2], b[1][3]};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bv, av, acc, FB, FA, 0, (int)scale_b, 0, (int)scale_a);
+}
+
+// The products of a wavefront's step: 32 codes a lane and fragment.
+template <bool WIDE, int FA, int FB, int MI, int NI>
+__device__ inline void multiply_step(const i32x4_t (&a)[MI][2], const uint32_t (&sca)[MI], const i32x4_t (&b)[NI][2], const uint32_t (&scb)[NI],
+                                     f32x16_t (&acc)[MI][NI])
+{
+    if constexpr (!WIDE) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = multiply32<FA, FB>(b[j], scb[j], a[i], sca[i], acc[i][j]);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            bf16x8_t wb[NI][2];
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const float s = __builtin_bit_cast(float, scb[j] << 23);
+                wb[j][0] = widen8<FB>(b[j][h][0], b[j][h][1], s);
+                wb[j][1] = widen8<FB>(b[j][h][2], b[j][h][3], s);
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const float s = __builtin_bit_cast(float, sca[i] << 23);
+                const bf16x8_t wa0 = widen8<FA>(a[i][h][0], a[i][h][1], s), wa1 = widen8<FA>(a[i][h][2], a[i][h][3], s);
+#pragma unroll
+                for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j][0], wa0, acc[i][j], 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j][1], wa1, acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i)           // (pins the products to this place)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) asm volatile("" : "+v"(acc[i][j]));
+}
+
+// A step's fragments, 4 KB apart in LDS, from a and b with their halves at a0 / a1 and b0 / b1; and their scales.  Every read of LDS
+// stands in one block with its wait: the compiler would put waits for the codes under way before them.
+__device__ inline void read_step(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, i32x4_t (&a)[4][2], i32x4_t (&b)[2][2])
+{
+    asm volatile("ds_read_b128 %0, %12\n\tds_read_b128 %1, %13\n\t"
+                 "ds_read_b128 %2, %12 offset:4096\n\tds_read_b128 %3, %13 offset:4096\n\t"
+                 "ds_read_b128 %4, %14\n\tds_read_b128 %5, %15\n\t"
+                 "ds_read_b128 %6, %14 offset:4096\n\tds_read_b128 %7, %15 offset:4096\n\t"
+                 "ds_read_b128 %8, %14 offset:8192\n\tds_read_b128 %9, %15 offset:8192\n\t"
+                 "ds_read_b128 %10, %14 offset:12288\n\tds_read_b128 %11, %15 offset:12288\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(b[0][0]), "=&v"(b[0][1]), "=&v"(b[1][0]), "=&v"(b[1][1]), "=&v"(a[0][0]), "=&v"(a[0][1]), "=&v"(a[1][0]),
+                   "=&v"(a[1][1]), "=&v"(a[2][0]), "=&v"(a[2][1]), "=&v"(a[3][0]), "=&v"(a[3][1])
+                 : "v"(b0), "v"(b1), "v"(a0), "v"(a1) : "memory");
+}
+__device__ inline void read_step(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, i32x4_t (&a)[2][2], i32x4_t (&b)[2][2])
+{
+    asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\t"
+                 "ds_read_b128 %2, %8 offset:4096\n\tds_read_b128 %3, %9 offset:4096\n\t"
+                 "ds_read_b128 %4, %10\n\tds_read_b128 %5, %11\n\t"
+                 "ds_read_b128 %6, %10 offset:4096\n\tds_read_b128 %7, %11 offset:4096\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(b[0][0]), "=&v"(b[0][1]), "=&v"(b[1][0]), "=&v"(b[1][1]), "=&v"(a[0][0]), "=&v"(a[0][1]), "=&v"(a[1][0]),
+                   "=&v"(a[1][1])
+                 : "v"(b0), "v"(b1), "v"(a0), "v"(a1) : "memory");
+}
+__device__ inline void read_scales(uint32_t at_a, uint32_t at_b, uint32_t (&a)[4], uint32_t (&b)[2])
+{
+    asm volatile("ds_read_u8 %0, %6\n\tds_read_u8 %1, %6 offset:128\n\tds_read_u8 %2, %6 offset:256\n\t"
+                 "ds_read_u8 %3, %6 offset:384\n\tds_read_u8 %4, %7\n\tds_read_u8 %5, %7 offset:128\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(b[0]), "=&v"(b[1]) : "v"(at_a), "v"(at_b) : "memory");
+}
+__device__ inline void read_scales(uint32_t at_a, uint32_t at_b, uint32_t (&a)[2], uint32_t (&b)[2])
+{
+    asm volatile("ds_read_u8 %0, %4\n\tds_read_u8 %1, %4 offset:128\n\tds_read_u8 %2, %5\n\tds_read_u8 %3, %5 offset:128\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(a[0]), "=&v"(a[1]), "=&v"(b[0]), "=&v"(b[1]) : "v"(at_a), "v"(at_b) : "memory");
+}
+
+// Nothing moves across: neither memory accesses nor matrix instructions.
+__device__ inline void phase_end()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// N consecutive outputs of a row.  PAST: a line that no other store completes, and nobody reads again soon.
+template <int N, bool PAST, class T, class V>
+__device__ inline void store_piece(T *out, const MmArgs &p, int split, int64_t i, int64_t j, const V v)
+{
+    if (i >= p.m || j >= p.n) return;
+    T *o = out + ((int64_t)split * p.m + i) * p.ldo + j;
+    if (j + N <= p.n) {
+        if (PAST) __builtin_nontemporal_store(v, reinterpret_cast<V *>(o));
+        else *reinterpret_cast<V *>(o) = v;
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < N; ++r)
+        if (j + r < p.n) o[r] = v[r];
+}
+
+// A workgroup's outputs turn in LDS, so that its rows leave whole: as they stand, a store would have 16 bytes of 32 rows.  PASSES
+// parts of a wavefront's rows after each other (fp32: room).  Pieces of 16 bytes are permuted by the row.  All wavefronts call it,
+// when nothing else of the LDS is in use.
+template <class T, bool PAST, int BM, int BN, int WM, int WN, int MI, int NI>
+__device__ inline void leave_as(const MmArgs &p, int split, int64_t m0, int64_t n0, const f32x16_t (&acc)[MI][NI], uint8_t *lds)
+{
+    constexpr int PASSES = sizeof(T) / 2, ROWS = BM / PASSES, PART = MI / PASSES, LINE = BN * sizeof(T), PIECES = LINE / 16;
+    constexpr int PER = 1024 / LINE, NW = WM * WN;           // rows of a wavefront's store
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l31 = lane & 31, half = lane >> 5;
+    const int wm = wave % WM, wn = wave / WM * (BN / WN);
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PART; ++i) {
+            uint8_t *line = lds + ((wm * PART + i) * 32 + l31) * LINE;
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x16_t &v = acc[pass * PART + i][j];
+                    const int byte = (wn + j * 32 + q * 8 + half * 4) * (int)sizeof(T);
+                    uint8_t *at = line + ((byte >> 4) ^ (l31 & 15)) * 16 + (byte & 15);
+                    if constexpr (sizeof(T) == 4) {
+                        *reinterpret_cast<f32x4_t *>(at) = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                    } else {
+                        uint32_t w[2];
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            w[r] = from_float<T>(v[4 * q + 2 * r]) | (uint32_t)from_float<T>(v[4 * q + 2 * r + 1]) << 16;
+                        *reinterpret_cast<uint2 *>(at) = make_uint2(w[0], w[1]);
+                    }
+                }
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int it = 0; it < ROWS / (NW * PER); ++it) {
+            const int lr = (it * NW + wave) * PER + lane / PIECES, c = (lane % PIECES) ^ (lr & 15);
+            const i32x4_t v = *reinterpret_cast<const i32x4_t *>(lds + lr * LINE + (lane % PIECES) * 16);
+            const int64_t row = m0 + (lr / (PART * 32)) * (BM / WM) + pass * (PART * 32) + lr % (PART * 32);
+            if constexpr (sizeof(T) == 4) store_piece<4, PAST>((float *)p.out, p, split, row, n0 + c * 4, __builtin_bit_cast(f4u_t, v));
+            else store_piece<8, PAST>((uint16_t *)p.out, p, 0, row, n0 + c * 8, __builtin_bit_cast(u16x8u_t, v));
+        }
+    }
+}
+template <int BM, int BN, int WM, int WN, int MI, int NI>
+__device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0, const f32x16_t (&acc)[MI][NI], uint8_t *lds)
+{
+    if (p.dtype == STX_F32) {
+        if (p.past) leave_as<float, true, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
+        else leave_as<float, false, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
+    } else if (p.dtype == STX_BF16) {
+        if (p.past) leave_as<bf16_t, true, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
+        else leave_as<bf16_t, false, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
+    } else {
+        leave_as<f16_t, false, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
+    }
+}
+
+// A BM x BN tile by WM x WN wavefronts, in 32 x 32 products.  A stage is one block of 128 columns: its codes go straight to LDS, a
+// row's 128 bytes in a line (requested as one), and a stage is multiplied in two steps of 64 columns while the next one's codes are
+// under way into the other buffer.  Piece c (16 bytes) of row r lies at c ^ (r / 2 % 8), and a lane reads pieces h and h + 2 of its
+// row's half, h = lane / 32: 2.86 ns a read and CU, as 64 lanes side by side; other orders 3.6 to 7.0.
+//
+// Four wavefronts: a workgroup takes half of a CU, so that one's outputs leave while the other multiplies.  Eight: two of them
+// share a SIMD, and the second runs one phase behind the first (it passes one more barrier at the start), so that one multiplies
+// while the other reads its fragments and requests codes:
+//
+//   phase      2t         2t + 1     2t + 2
+//   group 0    read t     multiply   read t + 1
+//   group 1    multiply   read t     multiply
+//
+// The other buffer is refilled from a stage's first step on, behind the barrier that follows the later group's last reads of it;
+// every wavefront waits for its own requests before the barrier in front of the next stage's first read.
 template <int BM, int BN, int WM, int WN, bool WIDE, int FA, int FB>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
 {
-    constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, LA = BM / 8 / NW, LB = BN / 8 / NW;
-    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "whole rounds of loads");
-    __shared__ __align__(16) uint8_t s_a0[BM * kBlock], s_a1[BM * kBlock], s_b0[BN * kBlock], s_b1[BN * kBlock];
-    __shared__ uint32_t s_scale[2][BM + BN];
+    constexpr int NW = WM * WN, MI = BM / WM / 32, NI = BN / WN / 32, LA = BM / 8 / NW, LB = BN / 8 / NW, BUF = (BM + BN) * kBlock;
+    constexpr bool PHASES = NW == 8;
+    static_assert(BM + BN == NW * 64 && 2 * BUF >= NW * MI * 4096, "a thread for each row's scales; room for the outputs");
+    __shared__ __align__(16) uint8_t s_buf[2 * BUF];
+    __shared__ uint32_t s_scale[2][BM + BN];                 // a word for four stages
     int tm, tn, split;
     tile_of(p, tm, tn, split);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int l15 = lane & 15, kg = lane >> 4;
+    const int l31 = lane & 31, half = lane >> 5, group = wave >> 2;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-    const int kb0 = split * p.kb_split, kb1 = min(kb0 + p.kb_split, p.nkb);
-    // loads: a wavefront's 64 pieces are 8 rows; rows behind the last one repeat it
-    static_assert(NW % 2 == 0, "a wavefront's rows begin at the same place of 16 in every round");
+    const int kb0 = split * p.kb_split, stages = min(kb0 + p.kb_split, p.nkb) - kb0;
+    // requests: a wavefront's 64 pieces are 8 rows; rows behind the last one repeat it
     const int piece = ((lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7)) * 16;
     uint32_t oa[LA], ob[LB];
 #pragma unroll
@@ -164,83 +343,74 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
 #pragma unroll
     for (int i = 0; i < LB; ++i) ob[i] = (uint32_t)(min((int64_t)((i * NW + wave) * 8 + (lane >> 3)), p.n - 1 - n0) * p.ldb) + piece;
     const uint8_t *ga = p.a + m0 * p.lda + (int64_t)kb0 * kBlock, *gb = p.b + n0 * p.ldb + (int64_t)kb0 * kBlock;
-    auto fetch = [&](uint8_t *sa, uint8_t *sb) {
+    auto fetch = [&](int buf) {
+        uint8_t *to = s_buf + buf * BUF + wave * 1024;
 #pragma unroll
-        for (int i = 0; i < LA; ++i)
-            __builtin_amdgcn_global_load_lds((global_ptr_t)(ga + oa[i]), (lds_ptr_t)(sa + (i * NW + wave) * 1024), 16, 0, 0);
+        for (int i = 0; i < LA; ++i) __builtin_amdgcn_global_load_lds((global_ptr_t)(ga + oa[i]), (lds_ptr_t)(to + i * NW * 1024), 16, 0, 0);
 #pragma unroll
         for (int i = 0; i < LB; ++i)
-            __builtin_amdgcn_global_load_lds((global_ptr_t)(gb + ob[i]), (lds_ptr_t)(sb + (i * NW + wave) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr_t)(gb + ob[i]), (lds_ptr_t)(to + BM * kBlock + i * NW * 1024), 16, 0, 0);
         ga += kBlock;
         gb += kBlock;
     };
-    // scales: a thread brings those of one row, a word for four steps, one group of steps ahead
-    const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-    static_assert(BM + BN == NW * 64, "a thread for each row's scales");
-    const uint8_t *scales = threadIdx.x < BM ? p.as + min(m0 + (int)threadIdx.x, p.m - 1) * p.ldas
-                                             : p.bs + min(n0 + (int)threadIdx.x - BM, p.n - 1) * p.ldbs;
-    uint32_t word = *reinterpret_cast<const uint32_t *>(scales + kb0);
-    s_scale[(kb0 >> 2) & 1][threadIdx.x] = word;
-    f32x4_t acc[MI][NI];
+    const uint8_t *gs = ((int)threadIdx.x < BM ? p.as + min(m0 + (int)threadIdx.x, p.m - 1) * p.ldas
+                                               : p.bs + min(n0 + (int)threadIdx.x - BM, p.n - 1) * p.ldbs) + kb0;
+    auto fetch_scales = [&](int to) {
+        __builtin_amdgcn_global_load_lds((global_ptr_t)gs, (lds_ptr_t)(s_scale[to] + wave * 64), 4, 0, 0);
+        gs += 4;
+    };
+    const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
+    const uint32_t at0 = l31 * kBlock + (half ^ ((l31 >> 1) & 7)) * 16;
+    const uint32_t at_a = (uint32_t)(uintptr_t)(lds_ptr_t)&s_buf[0] + wm * kBlock + at0;
+    const uint32_t at_b = (uint32_t)(uintptr_t)(lds_ptr_t)&s_buf[0] + (BM + wn) * kBlock + at0;
+    const uint32_t lds_scale = (uint32_t)(uintptr_t)(lds_ptr_t)&s_scale[0][0];
+    const uint32_t at_sa = lds_scale + 4 * (wm + l31), at_sb = lds_scale + 4 * (BM + wn + l31);
+    f32x16_t acc[MI][NI];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < NI; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    const int at0 = l15 * kBlock + (kg ^ (l15 >> 1)) * 16, at1 = l15 * kBlock + ((kg + 4) ^ (l15 >> 1)) * 16;
-    auto compute = [&](const uint8_t *sa, const uint8_t *sb, int kb) {
-        const uint8_t *sc = reinterpret_cast<const uint8_t *>(s_scale[(kb >> 2) & 1]) + (kb & 3);
-        uint32_t scb[NI], sca[MI];
+        for (int j = 0; j < NI; ++j)
 #pragma unroll
-        for (int j = 0; j < NI; ++j) scb[j] = sc[4 * (BM + wn + j * 16 + l15)];
-#pragma unroll
-        for (int i = 0; i < MI; ++i) sca[i] = sc[4 * (wm + i * 16 + l15)];
-#pragma unroll
-        for (int half = 0; half < (WIDE ? 2 : 1); ++half) {
-            Frag<WIDE, FB> fb[NI];
-#pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                Piece<WIDE> q;
-                q.load(sb + (wn + j * 16) * kBlock, at0, at1, half);
-                fb[j].set(q, scb[j]);
-            }
-            Piece<WIDE> next;
-            next.load(sa + wm * kBlock, at0, at1, half);
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                Frag<WIDE, FA> fa;
-                fa.set(next, sca[i]);
-                if (i + 1 < MI) next.load(sa + (wm + (i + 1) * 16) * kBlock, at0, at1, half);
-#pragma unroll
-                for (int j = 0; j < NI; ++j) acc[i][j] = multiply<FA, FB>(fb[j], fa, acc[i][j]);
-                __builtin_amdgcn_sched_barrier(0);           // no fragments of later rows ahead of these: registers
-            }
-        }
-    };
-    // the next group's scales: fetched in its first step, in LDS two steps later (read by nobody since the group before)
-    auto scales_ahead = [&](int kb) {
-        if ((kb & 3) == 0 && kb + 4 < kb1) word = *reinterpret_cast<const uint32_t *>(scales + kb + 4);
-        if ((kb & 3) == 2) s_scale[((kb >> 2) + 1) & 1][threadIdx.x] = word;
-    };
-    auto arrive = [&]() {                  // this step's loads have come, and every wavefront is done with the other buffer
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    uint32_t sca[MI], scb[NI];
+    fetch_scales(0);
+    fetch(0);
+    if constexpr (PHASES) {
         __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0)
-        __syncthreads();
-    };
-    fetch(s_a0, s_b0);
-    for (int kb = kb0; kb < kb1; kb += 2) {
-        arrive();
-        if (kb + 1 < kb1) fetch(s_a1, s_b1);
-        scales_ahead(kb);
-        compute(s_a0, s_b0, kb);
-        if (kb + 1 < kb1) {                // (not a break: the accumulators stay where they are)
-            arrive();
-            if (kb + 2 < kb1) fetch(s_a0, s_b0);
-            compute(s_a1, s_b1, kb + 1);
+        phase_end();
+        if (group == 1) phase_end();
+    }
+    for (int s = 0; s < stages; ++s) {
+        if constexpr (!PHASES) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+            phase_end();
+        }
+        if (s + 1 < stages) fetch((s + 1) & 1);
+        if ((s & 3) == 0 && s + 4 < stages) fetch_scales(((s >> 2) + 1) & 1);
+        const uint32_t fa = at_a + (s & 1) * BUF, fb = at_b + (s & 1) * BUF, from = ((s >> 2) & 1) * ((BM + BN) * 4) + (s & 3);
+        i32x4_t a[MI][2], b[NI][2];
+        read_step(fa, fa ^ 32u, fb, fb ^ 32u, a, b);
+        read_scales(at_sa + from, at_sb + from, sca, scb);
+        if constexpr (PHASES) phase_end();
+        __builtin_amdgcn_s_setprio(1);
+        multiply_step<WIDE, FA, FB, MI, NI>(a, sca, b, scb, acc);
+        __builtin_amdgcn_s_setprio(0);
+        if constexpr (PHASES) phase_end();
+        read_step(fa ^ 64u, fa ^ 96u, fb ^ 64u, fb ^ 96u, a, b);
+        if constexpr (PHASES) {
+            if (group == 1) __builtin_amdgcn_s_waitcnt(0x0f70);
+            phase_end();
+        }
+        __builtin_amdgcn_s_setprio(1);
+        multiply_step<WIDE, FA, FB, MI, NI>(a, sca, b, scb, acc);
+        __builtin_amdgcn_s_setprio(0);
+        if constexpr (PHASES) {
+            if (group == 0) __builtin_amdgcn_s_waitcnt(0x0f70);
+            phase_end();
         }
     }
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j) store4(p, split, m0 + wm + i * 16 + l15, n0 + wn + j * 16 + kg * 4, acc[i][j]);
+    if (PHASES && group == 0) phase_end();
+    leave<BM, BN, WM, WN>(p, split, m0, n0, acc, s_buf);
 }
 
 // The slices' sums, joined in order.
@@ -424,7 +594,13 @@ stx_status launch_q8_matmul(stx_ctx *c, const stx_q8 *a, const stx_q8 *b, int dt
 {
     const MmPlan t = mm_plan(a->rows, b->rows, a->cols);
     MmArgs p{a->codes, a->scales, b->codes, b->scales, a->ld, a->ld_scale, b->ld, b->ld_scale, a->rows, b->rows,
-             (int)((a->cols + kBlock - 1) / kBlock), t.kb_split, t.splits, (int)t.ntm, (int)t.ntn, out, ldo, dtype};
+             (int)((a->cols + kBlock - 1) / kBlock), t.kb_split, t.splits, (int)t.ntm, (int)t.ntn, out, ldo, dtype, 0};
+    // Outputs beyond the caches go past them, 4,096 x 14,848 bf16 over 1,024 columns in 79 us in place of 105.  Rows that are not
+    // whole lines leave parts of lines, which meet in the caches only where tiles are short (4,096 x 14,951: over 1,024 columns 93 us
+    // past the caches and 98 through them, over 128 columns 51 and 48).
+    const int64_t size = dtype == STX_F32 ? 4 : 2;
+    const bool lines = ldo * size % 128 == 0 && (uintptr_t)out % 128 == 0;
+    p.past = t.splits == 1 && p.m * p.n * size >= ((int64_t)64 << 20) && (lines || p.nkb >= 8);
     if (t.splits > 1) {
         p.out = work;
         p.ldo = p.n;

@@ -131,7 +131,7 @@ def check_product(got, x, y, dtype, cols):
 SIZES = [(1, 1, 1), (1, 17, 128), (2, 300, 129), (16, 16, 256), (17, 33, 1000), (5, 1500, 1024), (31, 700, 384), (64, 64, 640), (65, 129, 127),
          (100, 500, 2048), (128, 256, 512), (129, 257, 513), (255, 511, 896), (300, 1000, 100), (520, 130, 1500), (1, 4000, 8192),
          (700, 90, 20000), (257, 1030, 4100), (9, 5000, 300), (5000, 9, 300), (4500, 16, 640), (27, 300_000, 128), (300_000, 3, 100),
-         (16, 270_000, 136)]
+         (16, 270_000, 136), (2000, 6200, 128), (3500, 3601, 200), (6145, 2049, 512), (3333, 4001, 1025), (2600, 5003, 1664)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
