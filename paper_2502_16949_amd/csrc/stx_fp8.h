@@ -21,6 +21,7 @@ typedef _Float16 f16_t;
 // Vectors at the alignment of their elements: the hardware takes any multiple of an element.
 typedef float f4u_t __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint16_t u16x8u_t __attribute__((ext_vector_type(8), aligned(2)));
+typedef uint32_t u32x4u_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32u_t __attribute__((aligned(1)));
 
 template <class T> __device__ inline float to_float(uint16_t bits);
@@ -36,38 +37,83 @@ __device__ inline int octet_pos(int blk, int l16, int j)
     return sizeof(T) == 4 ? blk * kBlock + (j >> 2) * 64 + 4 * l16 + (j & 3) : blk * kBlock + 8 * l16 + j;
 }
 
-// Elements of an octet of a row of n elements as floats; 0 behind the row's end.
+// An octet as it lies in memory.  Requesting one and making floats of it are two functions, and a kernel requests all that it needs
+// first.  Nothing in a request depends on the row's end but its address: an access that would reach behind the end is moved back to
+// end there, and its elements are shifted into place when they are made floats, by wavefronts that hold such a one (a branch around
+// the request would make the kernel wait for it at the branch's end).
+template <class T> struct Octet { uint32_t w[sizeof(T) * 2]; };
+
+// The octet that lane l16 of block blk owns of a row of n elements (n >= 0).
 template <class T>
-__device__ inline void load_octet(const T *row, int blk, int l16, int64_t n, float (&v)[8])
+__device__ inline Octet<T> request_octet(const T *row, int blk, int l16, int64_t n)
 {
+    Octet<T> o;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int64_t at = (int64_t)blk * kBlock + h * 64 + 4 * l16;
-            if (at + 4 <= n) {
-                const f4u_t q = *reinterpret_cast<const f4u_t *>(row + at);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[4 * h + j] = q[j];
+            f4u_t q = {0.f, 0.f, 0.f, 0.f};
+            if (n >= 4) {
+                q = *reinterpret_cast<const f4u_t *>(row + min(at, n - 4));
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[4 * h + j] = at + j < n ? (float)row[at + j] : 0.f;
+                for (int j = 0; j < 3; ++j)
+                    if (at + j < n) q[j] = row[at + j];
+                __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0) here, and not in front of the other branch's request
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float f = q[j];      // (a bit cast of a vector's element itself takes the first one)
+                o.w[4 * h + j] = __builtin_bit_cast(uint32_t, f);
             }
         }
     } else {
         const uint16_t *r16 = reinterpret_cast<const uint16_t *>(row);
         const int64_t at = (int64_t)blk * kBlock + 8 * l16;
-        if (at + 8 <= n) {
-            const u16x8u_t q = *reinterpret_cast<const u16x8u_t *>(r16 + at);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = to_float<T>(q[j]);
+        u32x4u_t q = {0u, 0u, 0u, 0u};
+        if (n >= 8) {
+            q = *reinterpret_cast<const u32x4u_t *>(r16 + min(at, n - 8));
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = at + j < n ? to_float<T>(r16[at + j]) : 0.f;
+            for (int j = 0; j < 7; ++j)
+                if (at + j < n) q[j / 2] |= (uint32_t)r16[at + j] << (16 * (j & 1));
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o.w[j] = q[j];
+    }
+    return o;
+}
+// N elements moved down by `by` places of 0 to N, zeros behind them.
+template <int N>
+__device__ inline void shift_down(float *v, int by)
+{
+#pragma unroll
+    for (int s = N; s >= 1; s >>= 1)
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = (by & s) ? (j + s < N ? v[j + s] : 0.f) : v[j];
+}
+// The elements of request_octet(row, blk, l16, n) as floats; 0 behind the row's end.
+template <class T>
+__device__ inline void octet_floats(const Octet<T> &o, int blk, int l16, int64_t n, float (&v)[8])
+{
+    constexpr int N = 16 / sizeof(T);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 4) v[j] = __builtin_bit_cast(float, o.w[j]);
+        else v[j] = to_float<T>((uint16_t)(o.w[j / 2] >> (16 * (j & 1))));
+    }
+    const int64_t last = octet_pos<T>(blk, l16, 8 - N);
+    if (n >= N && __ballot(last + N > n)) {
+#pragma unroll
+        for (int h = 0; h < 8 / N; ++h) {
+            const int64_t over = octet_pos<T>(blk, l16, h * N) + N - n;
+            shift_down<N>(v + h * N, (int)(over < 0 ? 0 : over > N ? N : over));
         }
     }
 }
 
-// The same of a row of floats, in the octets of T: a weight goes with the rows that it scales.
+// Of a row of floats, in the octets of T: a weight goes with the rows that it scales.
 template <class T>
 __device__ inline void load_octet_as(const float *row, int blk, int l16, int64_t n, float (&v)[8])
 {

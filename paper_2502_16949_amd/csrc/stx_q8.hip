@@ -18,7 +18,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_rows(const T *__restrict__ x, i
     if (row >= rows) return;
     const int blk = (int)(i - row * blocks);
     float v[8];
-    load_octet<T>(x + row * ld, blk, l16, cols, v);
+    octet_floats(request_octet(x + row * ld, blk, l16, cols), blk, l16, cols, v);
     store_q8_octet<T, FORMAT>(q, row, blk, l16, v);
 }
 
@@ -33,14 +33,12 @@ __global__ __launch_bounds__(kThreads) void k_q8_turn(const T *__restrict__ x, i
     const int l16 = threadIdx.x & 15, rg = threadIdx.x >> 4, wave = threadIdx.x >> 6;
     const int row_blk = (int)(blockIdx.x / (unsigned)col_blocks), blk = (int)(blockIdx.x % (unsigned)col_blocks);
     const int64_t row0 = (int64_t)row_blk * kBlock + rg * 8;
+    Octet<T> raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i] = request_octet(x + (row0 + i) * ld, blk, l16, row0 + i < rows ? cols : 0);
     float v[8][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (row0 + i < rows) load_octet<T>(x + (row0 + i) * ld, blk, l16, cols, v[i]);
-        else
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-    }
+    for (int i = 0; i < 8; ++i) octet_floats(raw[i], blk, l16, row0 + i < rows ? cols : 0, v[i]);
     if (q.codes) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
