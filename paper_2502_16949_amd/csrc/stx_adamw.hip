@@ -142,16 +142,6 @@ __device__ inline void quad_noise(uint64_t seed, uint64_t at, uint32_t *m, uint3
     }
 }
 
-__device__ inline f4u_t load_grad(const void *g, int dtype, int64_t at)
-{
-    if (dtype == STX_F32) return *reinterpret_cast<const f4u_t *>((const float *)g + at);
-    typedef uint16_t u16x4u_t __attribute__((ext_vector_type(4), aligned(2)));
-    const u16x4u_t b = *reinterpret_cast<const u16x4u_t *>((const uint16_t *)g + at);
-    f4u_t v;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = dtype == STX_BF16 ? to_float<bf16_t>(b[j]) : to_float<f16_t>(b[j]);
-    return v;
-}
 __device__ inline float load_grad1(const void *g, int dtype, int64_t at)
 {
     if (dtype == STX_F32) return ((const float *)g)[at];
@@ -159,7 +149,30 @@ __device__ inline float load_grad1(const void *g, int dtype, int64_t at)
     return dtype == STX_BF16 ? to_float<bf16_t>(b) : to_float<f16_t>(b);
 }
 
-// A thread's octets: two quads of a block, 64 elements apart (stx_fp8.h).
+// A thread's octets: two quads of a block, 64 elements apart (stx_fp8.h).  Its gradients; 0 for a quad that the end cuts.
+template <class T>
+__device__ inline void load_grads(const AdamTensorArg &t, int64_t blk0, int l16, float (&g)[kAdamOctets][8])
+{
+    typedef uint16_t u16x4u_t __attribute__((ext_vector_type(4), aligned(2)));
+    using Quad = typename std::conditional<sizeof(T) == 4, f4u_t, u16x4u_t>::type;
+    Quad q[kAdamOctets][2];
+#pragma unroll
+    for (int o = 0; o < kAdamOctets; ++o)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t at = (blk0 + o * (kThreads / 16)) * kBlock + h * 64 + 4 * l16;
+            q[o][h] = Quad{};
+            if (at + 4 <= t.n) q[o][h] = *reinterpret_cast<const Quad *>((const T *)t.g + at);
+        }
+#pragma unroll
+    for (int o = 0; o < kAdamOctets; ++o)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (sizeof(T) == 4) g[o][j] = q[o][j / 4][j & 3];
+            else g[o][j] = to_float<T>(q[o][j / 4][j & 3]);
+        }
+}
+
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void k_adamw_tensors(AdamTensorsArgs a)
 {
@@ -175,53 +188,76 @@ __global__ __launch_bounds__(kThreads) void k_adamw_tensors(AdamTensorsArgs a)
     const int l16 = threadIdx.x & 15;
     const int64_t blk0 = (int64_t)(blockIdx.x - t.first) * (kAdamTile / kBlock) + (threadIdx.x >> 4);
     constexpr int O = kAdamOctets;
-    float p[O][8], m[O][8], v[O][8], g[O][8];
+    using Raw = typename std::conditional<BITS == 32, f4u_t, uint32_t>::type;
+    f4u_t pq[O][2];                        // requested first, all of them; a conversion beside a load would wait for it
+    Raw mq[O][2], vq[O][2];
+    float msq[O], vsq[O];
 #pragma unroll
     for (int o = 0; o < O; ++o) {
         const int64_t blk = blk0 + o * (kThreads / 16);
-        float ms = 0.f, vs = 0.f;
-        if (BITS == 8 && blk * kBlock < t.n) { ms = t.ms[blk]; vs = t.vs[blk]; }
+        msq[o] = vsq[o] = 0.f;
+        if (BITS == 8 && blk * kBlock < t.n) { msq[o] = t.ms[blk]; vsq[o] = t.vs[blk]; }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int64_t at = blk * kBlock + h * 64 + 4 * l16;
+            pq[o][h] = f4u_t{0.f, 0.f, 0.f, 0.f};
+            mq[o][h] = Raw{};
+            vq[o][h] = Raw{};
             if (at + 4 <= t.n) {
-                const f4u_t pq = *reinterpret_cast<const f4u_t *>(t.p + at), gq = load_grad(t.g, t.g_dtype, at);
-                float mq[4], vq[4];
+                pq[o][h] = *reinterpret_cast<const f4u_t *>(t.p + at);
                 if constexpr (BITS == 32) {
-                    const f4u_t a4 = *reinterpret_cast<const f4u_t *>((const float *)t.m + at), b4 = *reinterpret_cast<const f4u_t *>((const float *)t.v + at);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) { mq[j] = a4[j]; vq[j] = b4[j]; }
+                    mq[o][h] = *reinterpret_cast<const f4u_t *>((const float *)t.m + at);
+                    vq[o][h] = *reinterpret_cast<const f4u_t *>((const float *)t.v + at);
                 } else {
-                    unpack4<STX_E4M3>(*reinterpret_cast<const u32u_t *>((const uint8_t *)t.m + at), mq);
-                    unpack4<STX_E5M2>(*reinterpret_cast<const u32u_t *>((const uint8_t *)t.v + at), vq);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    p[o][4 * h + j] = pq[j];
-                    g[o][4 * h + j] = gq[j];
-                    m[o][4 * h + j] = BITS == 8 ? mq[j] * ms : mq[j];
-                    v[o][4 * h + j] = BITS == 8 ? vq[j] * vs : vq[j];
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bool in = at + j < t.n;
-                    p[o][4 * h + j] = in ? t.p[at + j] : 0.f;
-                    g[o][4 * h + j] = in ? load_grad1(t.g, t.g_dtype, at + j) : 0.f;
-                    if constexpr (BITS == 32) {
-                        m[o][4 * h + j] = in ? ((const float *)t.m)[at + j] : 0.f;
-                        v[o][4 * h + j] = in ? ((const float *)t.v)[at + j] : 0.f;
-                    } else {
-                        float x[4];
-                        unpack4<STX_E4M3>(in ? ((const uint8_t *)t.m)[at + j] : 0u, x);
-                        m[o][4 * h + j] = in ? x[0] * ms : 0.f;
-                        unpack4<STX_E5M2>(in ? ((const uint8_t *)t.v)[at + j] : 0u, x);
-                        v[o][4 * h + j] = in ? x[0] * vs : 0.f;
-                    }
+                    mq[o][h] = *reinterpret_cast<const u32u_t *>((const uint8_t *)t.m + at);
+                    vq[o][h] = *reinterpret_cast<const u32u_t *>((const uint8_t *)t.v + at);
                 }
             }
         }
     }
+    float p[O][8], m[O][8], v[O][8], g[O][8];
+    if (t.g_dtype == STX_F32) load_grads<float>(t, blk0, l16, g);
+    else if (t.g_dtype == STX_BF16) load_grads<bf16_t>(t, blk0, l16, g);
+    else load_grads<f16_t>(t, blk0, l16, g);
+#pragma unroll
+    for (int o = 0; o < O; ++o)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float *pp = &p[o][4 * h], *mp = &m[o][4 * h], *vp = &v[o][4 * h];
+            if constexpr (BITS == 8) {
+                unpack4<STX_E4M3>(mq[o][h], mp);
+                unpack4<STX_E5M2>(vq[o][h], vp);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                pp[j] = pq[o][h][j];
+                if constexpr (BITS == 32) { mp[j] = mq[o][h][j]; vp[j] = vq[o][h][j]; }
+                else { mp[j] *= msq[o]; vp[j] *= vsq[o]; }
+            }
+        }
+    // the end of a tensor of n % 4 != 0 elements, one lane of the tensor
+#pragma unroll
+    for (int o = 0; o < O; ++o)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t at = (blk0 + o * (kThreads / 16)) * kBlock + h * 64 + 4 * l16;
+            if (at >= t.n || at + 4 <= t.n) continue;
+            for (int j = 0; j < 3; ++j) {
+                if (at + j >= t.n) continue;
+                p[o][4 * h + j] = t.p[at + j];
+                g[o][4 * h + j] = load_grad1(t.g, t.g_dtype, at + j);
+                if constexpr (BITS == 32) {
+                    m[o][4 * h + j] = ((const float *)t.m)[at + j];
+                    v[o][4 * h + j] = ((const float *)t.v)[at + j];
+                } else {
+                    float x[4];
+                    unpack4<STX_E4M3>(((const uint8_t *)t.m)[at + j], x);
+                    m[o][4 * h + j] = x[0] * msq[o];
+                    unpack4<STX_E5M2>(((const uint8_t *)t.v)[at + j], x);
+                    v[o][4 * h + j] = x[0] * vsq[o];
+                }
+            }
+        }
     const uint64_t seed = BITS == 8 ? tensor_seed(k.seed, step, a.first_tensor + which) : 0;
 #pragma unroll
     for (int o = 0; o < O; ++o) {

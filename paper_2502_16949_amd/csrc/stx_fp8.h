@@ -210,7 +210,7 @@ __device__ inline uint32_t pack4(float a, float b, float c, float d)
     return (uint32_t)w;
 }
 template <int FORMAT>
-__device__ inline void unpack4(uint32_t w, float (&v)[4])
+__device__ inline void unpack4(uint32_t w, float *v)
 {
     typedef float f2 __attribute__((ext_vector_type(2)));
     f2 lo, hi;
