@@ -378,7 +378,8 @@ stx_status stx_q8_matmul(stx_ctx *ctx, const stx_q8 *a, const stx_q8 *b, int32_t
 /* AdamW, step number t:
  *   g' = g * grad_scale;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;
  *   p = p - lr weight_decay p;  p = p - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32, every operation rounded once, the numbers that no element changes formed in double.
+ * in fp32, every operation rounded once, but the root and the quotient, each within a unit of the last place; the
+ * numbers that no element changes are formed in double.  eps: 0, or from 2^-126 to 2^126.
  * bits: 32 (m and v are fp32) or 8.  In 8 bits m is held in STX_E4M3 and v in STX_E5M2 codes, with an fp32 scale for
  * each block of 128 elements: its largest magnitude over the format's largest number, or 0, with codes of 0, where that
  * magnitude is below 2^-100.  Values are rounded up or down by random bits, so that what a step adds is kept on the

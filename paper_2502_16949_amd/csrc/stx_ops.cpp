@@ -30,7 +30,8 @@ stx_status check_adamw(const stx_adamw *h)
     if (!h) return STX_ERR_NULL;
     if (h->bits != 32 && h->bits != 8) return STX_ERR_BAD_ARG;
     if (!(h->lr == h->lr) || !(h->weight_decay == h->weight_decay)) return STX_ERR_BAD_ARG;
-    if (!(h->beta1 >= 0.0 && h->beta1 < 1.0) || !(h->beta2 >= 0.0 && h->beta2 < 1.0) || !(h->eps >= 0.0)) return STX_ERR_BAD_ARG;
+    if (!(h->beta1 >= 0.0 && h->beta1 < 1.0) || !(h->beta2 >= 0.0 && h->beta2 < 1.0) ||
+        !(h->eps == 0.0 || (h->eps >= 0x1p-126 && h->eps <= 0x1p126))) return STX_ERR_BAD_ARG;
     if (!h->step_dev && h->step < 1) return STX_ERR_BAD_ARG;
     if (!aligned(h->step_dev, 8) || !aligned(h->grad_scale, 4)) return STX_ERR_BAD_ARG;
     return STX_OK;
