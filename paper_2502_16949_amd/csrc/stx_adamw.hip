@@ -84,14 +84,19 @@ __device__ inline uint64_t tensor_seed(uint64_t seed, uint64_t step, int tensor)
     return splitmix64_at(seed, (step << 16) + (uint64_t)tensor);
 }
 
-// One element; every operation rounded once (contraction is off).
+// One element; every operation rounded once (contraction is off), but the root and the quotient: the instructions
+// v_sqrt_f32 and v_rcp_f32 are within a unit of the last place, so the step is within 3 of them, and far below p's own rounding
+// when it is small against p.  (Rounded right they take some 25 instructions more: 4,000,000 x 128 in 8 bits 1,469 us, so
+// 1,320.)  Both want normal numbers: a small v is scaled, and the host has checked eps.
 __device__ inline void adam_element(const AdamCoef &k, float decay, bool scale_g, float &p, float g, float &m, float &v)
 {
     if (scale_g) g = g * k.gscale;
     m = m * k.b1 + g * k.om1;
     v = v * k.b2 + (g * g) * k.om2;
     p = p - p * decay;
-    p = p - (m * k.size) / (sqrtf(v) * k.root + k.eps);
+    const bool small = v < 0x1p-96f;
+    const float root = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? k.root * 0x1p-32f : k.root);
+    p = p - (m * k.size) * __builtin_amdgcn_rcpf(root + k.eps);
 }
 
 // x >= 0 to a format that keeps 23 - DROP bits of the mantissa, up or down by 16 random bits.  The steps below the smallest
@@ -344,27 +349,44 @@ __device__ inline void adam_row(const AdamCoef &k, uint64_t step, bool scale_g, 
 {
     const int blocks = (t.d4 + 31) / 32;
     const int64_t base = row * t.d4 * 4;
+    using Raw = typename std::conditional<BITS == 32, float4, uint32_t>::type;
+    float4 pq[ITERS], gq[ITERS];           // requested first, all of them; lanes behind the row's end request its last float4
+    Raw mq[ITERS], vq[ITERS];
+    float msq[ITERS], vsq[ITERS];
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it) {
+        const int q = min(lig + it * LPR, t.d4 - 1);
+        const int64_t at = base + 4 * q;
+        pq[it] = ld4(t.p + at);
+        gq[it] = ld4_stream(grad + 4 * q);
+        if constexpr (BITS == 32) {
+            mq[it] = ld4((const float *)t.m + at);
+            vq[it] = ld4((const float *)t.v + at);
+        } else {
+            mq[it] = *reinterpret_cast<const uint32_t *>((const uint8_t *)t.m + at);
+            vq[it] = *reinterpret_cast<const uint32_t *>((const uint8_t *)t.v + at);
+            msq[it] = t.ms[row * blocks + q / 32];
+            vsq[it] = t.vs[row * blocks + q / 32];
+        }
+    }
     float p[ITERS][4], m[ITERS][4], v[ITERS][4], g[ITERS][4];
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-        const int q = lig + it * LPR;
-        const bool in = q < t.d4;
-        const int64_t at = base + 4 * q;
-        const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float4 p4 = in ? ld4(t.p + at) : z, g4 = in ? ld4_stream(grad + 4 * q) : z;
-        p[it][0] = p4.x; p[it][1] = p4.y; p[it][2] = p4.z; p[it][3] = p4.w;
-        g[it][0] = g4.x; g[it][1] = g4.y; g[it][2] = g4.z; g[it][3] = g4.w;
+        p[it][0] = pq[it].x; p[it][1] = pq[it].y; p[it][2] = pq[it].z; p[it][3] = pq[it].w;
+        g[it][0] = gq[it].x; g[it][1] = gq[it].y; g[it][2] = gq[it].z; g[it][3] = gq[it].w;
         if constexpr (BITS == 32) {
-            const float4 m4 = in ? ld4((const float *)t.m + at) : z, v4 = in ? ld4((const float *)t.v + at) : z;
-            m[it][0] = m4.x; m[it][1] = m4.y; m[it][2] = m4.z; m[it][3] = m4.w;
-            v[it][0] = v4.x; v[it][1] = v4.y; v[it][2] = v4.z; v[it][3] = v4.w;
+            m[it][0] = mq[it].x; m[it][1] = mq[it].y; m[it][2] = mq[it].z; m[it][3] = mq[it].w;
+            v[it][0] = vq[it].x; v[it][1] = vq[it].y; v[it][2] = vq[it].z; v[it][3] = vq[it].w;
         } else {
-            const int64_t blk = row * blocks + q / 32;
-            const float ms = in ? t.ms[blk] : 0.f, vs = in ? t.vs[blk] : 0.f;
-            unpack4<STX_E4M3>(in ? *reinterpret_cast<const uint32_t *>((const uint8_t *)t.m + at) : 0u, m[it]);
-            unpack4<STX_E5M2>(in ? *reinterpret_cast<const uint32_t *>((const uint8_t *)t.v + at) : 0u, v[it]);
+            const bool in = lig + it * LPR < t.d4;           // (the others' moments are 0: no block's largest is among them)
+            unpack4<STX_E4M3>(mq[it], m[it]);
+            unpack4<STX_E5M2>(vq[it], v[it]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { m[it][j] *= ms; v[it][j] *= vs; }
+            for (int j = 0; j < 4; ++j) {
+                m[it][j] = in ? m[it][j] * msq[it] : 0.f;
+                v[it][j] = in ? v[it][j] * vsq[it] : 0.f;
+                g[it][j] = in ? g[it][j] : 0.f;
+            }
         }
     }
     float ss = 0.f;
