@@ -10,7 +10,8 @@
 //   (The unscaled 8-bit instructions cut in the same place.)
 //
 //   fp32 outputs: codes become bfloat16 times their power of two (v_cvt_scalef32_pk_bf16_*: exact, two codes an instruction) in
-//   front of v_mfma_f32_16x16x32_bf16, whose products are whole: 1e-7 of the result, at half the rate.
+//   front of v_mfma_f32_*_bf16, whose products are whole: 1e-7 of the result, at half the rate.  The conversions go on beside the
+//   matrix instructions (three to one of 32 x 32 x 16 make it 5 % longer).
 #include "stx_device.h"
 #include "stx_ops.h"
 
@@ -36,8 +37,6 @@ struct MmArgs {
     int past;                              // rows of out are whole lines
 };
 
-// One fragment of an operand: 32 codes a lane, of row lane % 16.  Which columns a lane holds does not matter to a sum as long as
-// both operands agree.
 template <int FORMAT>
 __device__ inline bf16x2_t widen2(int w, float scale, bool hi)
 {
@@ -52,52 +51,8 @@ __device__ inline bf16x8_t widen8(int lo, int hi, float scale)
     return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A piece is what one pass over a step takes of a row: all 32 codes of a lane, or, widened, half of them at a time (registers).
-template <bool WIDE> struct Piece;
-template <> struct Piece<false> {
-    i32x4_t lo, hi;
-    __device__ void load(const uint8_t *row, int at0, int at1, int)
-    {
-        lo = *reinterpret_cast<const i32x4_t *>(row + at0);
-        hi = *reinterpret_cast<const i32x4_t *>(row + at1);
-    }
-};
-template <> struct Piece<true> {
-    i32x4_t lo;
-    __device__ void load(const uint8_t *row, int at0, int at1, int half) { lo = *reinterpret_cast<const i32x4_t *>(row + (half ? at1 : at0)); }
-};
-template <bool WIDE, int FORMAT> struct Frag;
-template <int FORMAT> struct Frag<false, FORMAT> {
-    i32x8_t v;
-    int scale;
-    __device__ void set(const Piece<false> &p, uint32_t byte)
-    {
-        v = i32x8_t{p.lo[0], p.lo[1], p.lo[2], p.lo[3], p.hi[0], p.hi[1], p.hi[2], p.hi[3]};
-        scale = (int)byte;
-    }
-};
-template <int FORMAT> struct Frag<true, FORMAT> {
-    bf16x8_t v[2];
-    __device__ void set(const Piece<true> &p, uint32_t byte)
-    {
-        const float s = __builtin_bit_cast(float, byte << 23);
-        v[0] = widen8<FORMAT>(p.lo[0], p.lo[1], s);
-        v[1] = widen8<FORMAT>(p.lo[2], p.lo[3], s);
-    }
-};
-// acc += B A^T: a lane has row lane % 16 of A and 4 consecutive rows of B.
-template <int FA, int FB>
-__device__ inline f32x4_t multiply(const Frag<false, FB> &b, const Frag<false, FA> &a, f32x4_t acc)
-{
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.v, a.v, acc, FB, FA, 0, b.scale, 0, a.scale);
-}
-template <int FA, int FB>
-__device__ inline f32x4_t multiply(const Frag<true, FB> &b, const Frag<true, FA> &a, f32x4_t acc)
-{
-#pragma unroll
-    for (int s = 0; s < 2; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[s], a.v[s], acc, 0, 0, 0);
-    return acc;
-}
+// A scale's value; bytes are 1 to 254.
+__device__ inline float power(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // Four consecutive outputs of a row.
 __device__ inline void store4(const MmArgs &p, int split, int64_t i, int64_t j, const f32x4_t v)
@@ -130,11 +85,11 @@ __device__ inline void tile_of(const MmArgs &p, int &tm, int &tn, int &split)
     const unsigned total = gridDim.x, die = blockIdx.x % kDies, each = total / kDies, more = total % kDies;
     const unsigned i = die * each + (die < more ? die : more) + blockIdx.x / kDies;
     const unsigned tiles = (unsigned)p.ntm * (unsigned)p.ntn;
-    split = (int)(i / tiles);
+    split = __builtin_amdgcn_readfirstlane((int)(i / tiles));
     const unsigned t = i % tiles, stripe = t / (unsigned)(kStripe * p.ntn), r = t % (unsigned)(kStripe * p.ntn);
     const unsigned first = stripe * kStripe, high = min((unsigned)kStripe, (unsigned)p.ntm - first);
-    tm = (int)(first + r % high);
-    tn = (int)(r / high);
+    tm = __builtin_amdgcn_readfirstlane((int)(first + r % high));
+    tn = __builtin_amdgcn_readfirstlane((int)(r / high));
 }
 
 typedef const __attribute__((address_space(1))) void *global_ptr_t;
@@ -150,34 +105,42 @@ __device__ inline f32x16_t multiply32(const i32x4_t *b, uint32_t scale_b, const 
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bv, av, acc, FB, FA, 0, (int)scale_b, 0, (int)scale_a);
 }
 
-// The products of a wavefront's step: 32 codes a lane and fragment.
-template <bool WIDE, int FA, int FB, int MI, int NI>
+// Conversions and scalars may cross, nothing else.
+__device__ inline void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }
+
+// The products of a wavefront's step: 32 codes a lane and fragment.  between(u) is called after each of 2 MI parts of them.
+template <bool WIDE, int FA, int FB, int MI, int NI, class F>
 __device__ inline void multiply_step(const i32x4_t (&a)[MI][2], const uint32_t (&sca)[MI], const i32x4_t (&b)[NI][2], const uint32_t (&scb)[NI],
-                                     f32x16_t (&acc)[MI][NI])
+                                     f32x16_t (&acc)[MI][NI], F between)
 {
+    static_assert(NI == 2, "parts");
     if constexpr (!WIDE) {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < NI; ++j) acc[i][j] = multiply32<FA, FB>(b[j], scb[j], a[i], sca[i], acc[i][j]);
+            for (int j = 0; j < NI; ++j) {
+                acc[i][j] = multiply32<FA, FB>(b[j], scb[j], a[i], sca[i], acc[i][j]);
+                between(i * NI + j);
+            }
     } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             bf16x8_t wb[NI][2];
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                const float s = __builtin_bit_cast(float, scb[j] << 23);
+                const float s = power(scb[j]);
                 wb[j][0] = widen8<FB>(b[j][h][0], b[j][h][1], s);
                 wb[j][1] = widen8<FB>(b[j][h][2], b[j][h][3], s);
             }
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
-                const float s = __builtin_bit_cast(float, sca[i] << 23);
+                const float s = power(sca[i]);
                 const bf16x8_t wa0 = widen8<FA>(a[i][h][0], a[i][h][1], s), wa1 = widen8<FA>(a[i][h][2], a[i][h][3], s);
 #pragma unroll
                 for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j][0], wa0, acc[i][j], 0, 0, 0);
 #pragma unroll
                 for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j][1], wa1, acc[i][j], 0, 0, 0);
+                between(h * MI + i);
             }
         }
     }
@@ -315,18 +278,20 @@ __device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0,
 // share a SIMD, and the second runs one phase behind the first (it passes one more barrier at the start), so that one multiplies
 // while the other reads its fragments and requests codes:
 //
-//   phase      2t         2t + 1     2t + 2
-//   group 0    read t     multiply   read t + 1
-//   group 1    multiply   read t     multiply
+//   phase      4s             4s + 1         4s + 2         4s + 3
+//   group 0    read 1st       multiply 1st   read 2nd       multiply 2nd
+//   group 1    multiply 2nd   read 1st       multiply 1st   read 2nd
 //
-// The other buffer is refilled from a stage's first step on, behind the barrier that follows the later group's last reads of it;
-// every wavefront waits for its own requests before the barrier in front of the next stage's first read.
+// (of stage s; group 1 still multiplies s - 1 in phase 4s).  A stage's codes of A are requested beside the first reads of the stage before,
+// when everybody has read their buffer, those of B, which only one group reads, between that group's products two stages before.
+// (All of them beside the reads made those phases the longest: 8,192 x 8,192 x 8,192 in 460 us.)  Every wavefront waits for its own
+// at the end of 4s + 3, before the first read of the next stage; group 0 leaves those in flight that it has just requested.
 template <int BM, int BN, int WM, int WN, bool WIDE, int FA, int FB>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
 {
     constexpr int NW = WM * WN, MI = BM / WM / 32, NI = BN / WN / 32, LA = BM / 8 / NW, LB = BN / 8 / NW, BUF = (BM + BN) * kBlock;
     constexpr bool PHASES = NW == 8;
-    static_assert(BM + BN == NW * 64 && 2 * BUF >= NW * MI * 4096, "a thread for each row's scales; room for the outputs");
+    static_assert(BM + BN <= NW * 64 && 2 * BUF >= NW * MI * 4096, "a thread for each row's scales; room for the outputs");
     __shared__ __align__(16) uint8_t s_buf[2 * BUF];
     __shared__ uint32_t s_scale[2][BM + BN];                 // a word for four stages
     int tm, tn, split;
@@ -335,28 +300,35 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
     const int l31 = lane & 31, half = lane >> 5, group = wave >> 2;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int kb0 = split * p.kb_split, stages = min(kb0 + p.kb_split, p.nkb) - kb0;
-    // requests: a wavefront's 64 pieces are 8 rows; rows behind the last one repeat it
+    // requests: a wavefront's 64 pieces are 8 rows, of B the rows that its group reads; rows behind the last one repeat it.  Offsets of
+    // 32 bits to a scalar base: a 64-bit sum in a vector register would wait until the other group's products are done
     const int piece = ((lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7)) * 16;
+    constexpr int NG = PHASES ? 4 : NW;    // wavefronts of a group
+    const int b_first = PHASES ? group * (BN / 16) + (wave & 3) : wave;         // in eights of rows
     uint32_t oa[LA], ob[LB];
 #pragma unroll
     for (int i = 0; i < LA; ++i) oa[i] = (uint32_t)(min((int64_t)((i * NW + wave) * 8 + (lane >> 3)), p.m - 1 - m0) * p.lda) + piece;
 #pragma unroll
-    for (int i = 0; i < LB; ++i) ob[i] = (uint32_t)(min((int64_t)((i * NW + wave) * 8 + (lane >> 3)), p.n - 1 - n0) * p.ldb) + piece;
+    for (int i = 0; i < LB; ++i) ob[i] = (uint32_t)(min((int64_t)((i * NG + b_first) * 8 + (lane >> 3)), p.n - 1 - n0) * p.ldb) + piece;
     const uint8_t *ga = p.a + m0 * p.lda + (int64_t)kb0 * kBlock, *gb = p.b + n0 * p.ldb + (int64_t)kb0 * kBlock;
-    auto fetch = [&](int buf) {
-        uint8_t *to = s_buf + buf * BUF + wave * 1024;
-#pragma unroll
-        for (int i = 0; i < LA; ++i) __builtin_amdgcn_global_load_lds((global_ptr_t)(ga + oa[i]), (lds_ptr_t)(to + i * NW * 1024), 16, 0, 0);
-#pragma unroll
-        for (int i = 0; i < LB; ++i)
-            __builtin_amdgcn_global_load_lds((global_ptr_t)(gb + ob[i]), (lds_ptr_t)(to + BM * kBlock + i * NW * 1024), 16, 0, 0);
-        ga += kBlock;
-        gb += kBlock;
+    auto request = [&](const uint8_t *from, uint32_t &at, uint8_t *to) {
+        asm volatile("" : "+v"(at));       // (keeps it 32 bits)
+        __builtin_amdgcn_global_load_lds((global_ptr_t)(from + at), (lds_ptr_t)to, 16, 0, 0);
     };
-    const uint8_t *gs = ((int)threadIdx.x < BM ? p.as + min(m0 + (int)threadIdx.x, p.m - 1) * p.ldas
-                                               : p.bs + min(n0 + (int)threadIdx.x - BM, p.n - 1) * p.ldbs) + kb0;
+    auto fetch_a = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < LA; ++i) request(ga, oa[i], s_buf + buf * BUF + (i * NW + wave) * 1024);
+        ga += kBlock;
+    };
+    auto fetch_b = [&](int buf, int i) { request(gb, ob[i], s_buf + buf * BUF + BM * kBlock + (i * NG + b_first) * 1024); };
+    const bool of_a = wave * 64 < BM;      // whose rows' scales this wavefront requests
+    const uint8_t *gs = (of_a ? p.as + m0 * p.ldas : p.bs + n0 * p.ldbs) + kb0;
+    uint32_t os = of_a ? (uint32_t)(min((int64_t)threadIdx.x, p.m - 1 - m0) * p.ldas)
+                             : (uint32_t)(min((int64_t)threadIdx.x - BM, p.n - 1 - n0) * p.ldbs);
     auto fetch_scales = [&](int to) {
-        __builtin_amdgcn_global_load_lds((global_ptr_t)gs, (lds_ptr_t)(s_scale[to] + wave * 64), 4, 0, 0);
+        if (wave * 64 >= BM + BN) return;
+        asm volatile("" : "+v"(os));
+        __builtin_amdgcn_global_load_lds((global_ptr_t)(gs + os), (lds_ptr_t)(s_scale[to] + wave * 64), 4, 0, 0);
         gs += 4;
     };
     const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
@@ -373,43 +345,64 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     uint32_t sca[MI], scb[NI];
+    i32x4_t a[MI][2], b[NI][2];
+    uint32_t fa = 0, fb = 0;
+    auto read_first = [&](int s) {
+        const uint32_t from = ((s >> 2) & 1) * ((BM + BN) * 4) + (s & 3);
+        fa = at_a + (s & 1) * BUF;
+        fb = at_b + (s & 1) * BUF;
+        read_step(fa, fa ^ 32u, fb, fb ^ 32u, a, b);
+        read_scales(at_sa + from, at_sb + from, sca, scb);
+    };
+    auto multiply = [&](auto between) {
+        __builtin_amdgcn_s_setprio(1);
+        multiply_step<WIDE, FA, FB, MI, NI>(a, sca, b, scb, acc, between);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    auto all_b = [&](int s) {              // stage s, or the last one again behind it (a branch would cost the sums' registers)
+#pragma unroll
+        for (int i = 0; i < LB; ++i) fetch_b(s & 1, i);
+        if (s + 1 < stages) gb += kBlock;
+    };
     fetch_scales(0);
-    fetch(0);
+    fetch_a(0);
+    all_b(0);
     if constexpr (PHASES) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0)
+        all_b(1);
+        __builtin_amdgcn_s_waitcnt(0x0f70 + LB);             // vmcnt(LB): all but stage 1's
         phase_end();
         if (group == 1) phase_end();
     }
     for (int s = 0; s < stages; ++s) {
         if constexpr (!PHASES) {
-            __builtin_amdgcn_s_waitcnt(0x0f70);
+            __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0)
             phase_end();
         }
-        if (s + 1 < stages) fetch((s + 1) & 1);
         if ((s & 3) == 0 && s + 4 < stages) fetch_scales(((s >> 2) + 1) & 1);
-        const uint32_t fa = at_a + (s & 1) * BUF, fb = at_b + (s & 1) * BUF, from = ((s >> 2) & 1) * ((BM + BN) * 4) + (s & 3);
-        i32x4_t a[MI][2], b[NI][2];
-        read_step(fa, fa ^ 32u, fb, fb ^ 32u, a, b);
-        read_scales(at_sa + from, at_sb + from, sca, scb);
+        if (s + 1 < stages) fetch_a((s + 1) & 1);
+        if (!PHASES && s + 1 < stages) all_b(s + 1);
+        read_first(s);
         if constexpr (PHASES) phase_end();
-        __builtin_amdgcn_s_setprio(1);
-        multiply_step<WIDE, FA, FB, MI, NI>(a, sca, b, scb, acc);
-        __builtin_amdgcn_s_setprio(0);
+        multiply([](int) {});
         if constexpr (PHASES) phase_end();
         read_step(fa ^ 64u, fa ^ 96u, fb ^ 64u, fb ^ 96u, a, b);
-        if constexpr (PHASES) {
+        if constexpr (!PHASES) multiply([](int) {});
+        else {
             if (group == 1) __builtin_amdgcn_s_waitcnt(0x0f70);
             phase_end();
-        }
-        __builtin_amdgcn_s_setprio(1);
-        multiply_step<WIDE, FA, FB, MI, NI>(a, sca, b, scb, acc);
-        __builtin_amdgcn_s_setprio(0);
-        if constexpr (PHASES) {
-            if (group == 0) __builtin_amdgcn_s_waitcnt(0x0f70);
+            multiply([&](int u) {
+                if (u % 2) return;
+                keep_order();
+                fetch_b(s & 1, u / 2);
+                keep_order();
+            });
+            if (s + 3 < stages) gb += kBlock;
+            if (group == 0) __builtin_amdgcn_s_waitcnt(0x0f70 + LB);
             phase_end();
         }
     }
     if (PHASES && group == 0) phase_end();
+    __builtin_amdgcn_s_waitcnt(0x0f70);
     leave<BM, BN, WM, WN>(p, split, m0, n0, acc, s_buf);
 }
 
@@ -468,23 +461,36 @@ __global__ __launch_bounds__(kThreads) void k_q8_direct(MmArgs p)
         }
         for (int kb = ks; kb < p.nkb; kb += KS) {
             const int at0 = kb * kBlock + kg * 16, at1 = at0 + 64;
-            Piece<false> qa[MI], qb[NI];
-            uint32_t ba[MI], bb[NI];
+            i32x4_t qa[MI][2], qb[NI][2];
+            float ba[MI], bb[NI];
 #pragma unroll
-            for (int j = 0; j < NI; ++j) { qb[j].load(rb[j], at0, at1, 0); bb[j] = sb[j][kb]; }
+            for (int j = 0; j < NI; ++j) {
+                qb[j][0] = *reinterpret_cast<const i32x4_t *>(rb[j] + at0);
+                qb[j][1] = *reinterpret_cast<const i32x4_t *>(rb[j] + at1);
+                bb[j] = power(sb[j][kb]);
+            }
 #pragma unroll
-            for (int i = 0; i < MI; ++i) { qa[i].load(ra[i], at0, at1, 0); ba[i] = sa[i][kb]; }
+            for (int i = 0; i < MI; ++i) {
+                qa[i][0] = *reinterpret_cast<const i32x4_t *>(ra[i] + at0);
+                qa[i][1] = *reinterpret_cast<const i32x4_t *>(ra[i] + at1);
+                ba[i] = power(sa[i][kb]);
+            }
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                Frag<true, FB> fb[NI];
+            for (int h = 0; h < 2; ++h) {
+                bf16x8_t wb[NI][2];
 #pragma unroll
-                for (int j = 0; j < NI; ++j) fb[j].set(Piece<true>{half ? qb[j].hi : qb[j].lo}, bb[j]);
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) wb[j][s] = widen8<FB>(qb[j][h][2 * s], qb[j][h][2 * s + 1], bb[j]);
 #pragma unroll
                 for (int i = 0; i < MI; ++i) {
-                    Frag<true, FA> fa;
-                    fa.set(Piece<true>{half ? qa[i].hi : qa[i].lo}, ba[i]);
+                    bf16x8_t wa[2];
 #pragma unroll
-                    for (int j = 0; j < NI; ++j) acc[i][j] = multiply<FA, FB>(fb[j], fa, acc[i][j]);
+                    for (int s = 0; s < 2; ++s) wa[s] = widen8<FA>(qa[i][h][2 * s], qa[i][h][2 * s + 1], ba[i]);
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][s], wa[s], acc[i][j], 0, 0, 0);
                 }
             }
         }
@@ -519,7 +525,7 @@ struct MmPlan {
     int64_t ntm, ntn;
     int splits, kb_split;
 };
-static MmPlan mm_plan(int64_t m, int64_t n, int64_t k)
+static MmPlan mm_plan(int64_t m, int64_t n, int64_t k, bool wide)
 {
     MmPlan t{};
     const int64_t nkb = (k + kBlock - 1) / kBlock, few = m < n ? m : n;
@@ -540,8 +546,13 @@ static MmPlan mm_plan(int64_t m, int64_t n, int64_t k)
         t.ntn = (n + 16 * t.ni - 1) / (16 * t.ni);
         return t;
     }
-    const int64_t big = ((m + 255) / 256) * ((n + 255) / 256);
-    t.bm = t.bn = big >= 192 ? 256 : 128;
+    // Tiles of 256 x 256 where they fill three quarters of the compute units (14,951 x 1,024 over 8,192 columns, 236 tiles, bf16: 130 us,
+    // in 128 x 128 142; 8,192 x 1,024 over 14,976, 128 tiles: 171 and 144).  Widened, where the matrix instructions take twice as long,
+    // 256 x 128 otherwise, if they do (the same sizes: 256 tiles in 193 us, in 256 x 256 259, in 128 x 128 234; without widening
+    // 151).  Below, tiles of 128 x 128, and the columns cut into slices until two workgroups for each compute unit are there.
+    auto tiles_of = [&](int64_t bm, int64_t bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
+    t.bm = tiles_of(256, 256) >= 192 || (wide && tiles_of(256, 128) >= 192) ? 256 : 128;
+    t.bn = tiles_of(256, 256) >= 192 ? 256 : 128;
     t.ntm = (m + t.bm - 1) / t.bm;
     t.ntn = (n + t.bn - 1) / t.bn;
     const int64_t tiles = t.ntm * t.ntn, room = t.bm == 256 ? 256 : 512;
@@ -557,8 +568,8 @@ static MmPlan mm_plan(int64_t m, int64_t n, int64_t k)
 size_t q8_matmul_work_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (m == 0 || n == 0) return 0;
-    const MmPlan t = mm_plan(m, n, k);
-    return t.splits > 1 ? ((size_t)t.splits * (size_t)m * (size_t)n * 4 + 255) / 256 * 256 : 0;
+    const int a = mm_plan(m, n, k, false).splits, b = mm_plan(m, n, k, true).splits, splits = a > b ? a : b;
+    return splits > 1 ? ((size_t)splits * (size_t)m * (size_t)n * 4 + 255) / 256 * 256 : 0;
 }
 
 template <int FA, int FB>
@@ -581,7 +592,9 @@ static void mm_go(stx_ctx *c, const MmPlan &t, bool wide, const MmArgs &p)
     }
     const dim3 grid((unsigned)(t.ntm * t.ntn * t.splits));
     ProfScope prof(c, "k_q8_mm");
-    if (t.bm == 256) {
+    if (t.bm != t.bn) {
+        hipLaunchKernelGGL((k_q8_mm<256, 128, 4, 2, true, FA, FB>), grid, dim3(512), 0, c->stream, p);
+    } else if (t.bm == 256) {
         if (wide) hipLaunchKernelGGL((k_q8_mm<256, 256, 2, 4, true, FA, FB>), grid, dim3(512), 0, c->stream, p);
         else hipLaunchKernelGGL((k_q8_mm<256, 256, 2, 4, false, FA, FB>), grid, dim3(512), 0, c->stream, p);
     } else {
@@ -592,7 +605,8 @@ static void mm_go(stx_ctx *c, const MmPlan &t, bool wide, const MmArgs &p)
 
 stx_status launch_q8_matmul(stx_ctx *c, const stx_q8 *a, const stx_q8 *b, int dtype, void *out, int64_t ldo, void *work)
 {
-    const MmPlan t = mm_plan(a->rows, b->rows, a->cols);
+    const bool wide = dtype == STX_F32;
+    const MmPlan t = mm_plan(a->rows, b->rows, a->cols, wide);
     MmArgs p{a->codes, a->scales, b->codes, b->scales, a->ld, a->ld_scale, b->ld, b->ld_scale, a->rows, b->rows,
              (int)((a->cols + kBlock - 1) / kBlock), t.kb_split, t.splits, (int)t.ntm, (int)t.ntn, out, ldo, dtype, 0};
     // Outputs beyond the caches go past them, 4,096 x 14,848 bf16 over 1,024 columns in 79 us in place of 105.  Rows that are not
@@ -606,7 +620,7 @@ stx_status launch_q8_matmul(stx_ctx *c, const stx_q8 *a, const stx_q8 *b, int dt
         p.ldo = p.n;
         p.dtype = STX_F32;
     }
-    const bool wide = dtype == STX_F32, ea = a->format == STX_E4M3, eb = b->format == STX_E4M3;
+    const bool ea = a->format == STX_E4M3, eb = b->format == STX_E4M3;
     if (ea && eb) mm_go<STX_E4M3, STX_E4M3>(c, t, wide, p);
     else if (ea) mm_go<STX_E4M3, STX_E5M2>(c, t, wide, p);
     else if (eb) mm_go<STX_E5M2, STX_E4M3>(c, t, wide, p);
