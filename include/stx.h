@@ -365,11 +365,12 @@ stx_status stx_q8_quantize(stx_ctx *ctx, int32_t dtype, int64_t rows, int64_t co
                            const stx_q8 *q, const stx_q8 *qt);
 
 /* out (a->rows x b->rows, `dtype`, ldo elements between rows) = A B^T over a->cols == b->cols columns (at least one), on
- * the matrix cores; sums are fp32, rounded once into out.  The formats of a and b may differ.  ld of both at most 2^24.
+ * the matrix cores; sums are fp32, rounded once into out.  The formats of a and b may differ.  ld and ld_scale at most 2^24.
  * For an fp32 out products are whole.  For a 16-bit out the 8-bit instructions sum them in eights and cut off what lies
  * below 2^-13 of the largest of an eight: far less than the output's own rounding, unless nearly all of a sum cancels.
  * out shares no memory with the operands.  work: stx_q8_matmul_work_bytes bytes, 256-byte aligned (products of few
- * tiles and long rows are cut along the rows and joined there, in a fixed order); null where that says 0.      */
+ * tiles and long rows are cut along the rows and joined there, in a fixed order); null where that says 0.  It is in use
+ * until the call's kernels have ended: calls on other streams, and graphs that run beside each other, need their own. */
 stx_status stx_q8_matmul_work_bytes(const stx_ctx *ctx, int64_t rows_a, int64_t rows_b, int64_t cols,
                                     size_t *bytes /* host, out */);
 stx_status stx_q8_matmul(stx_ctx *ctx, const stx_q8 *a, const stx_q8 *b, int32_t dtype, void *out, int64_t ldo,

@@ -131,7 +131,8 @@ stx_status stx_q8_matmul(stx_ctx *ctx, const stx_q8 *a, const stx_q8 *b, int32_t
     if (s != STX_OK) return s;
     if (a->cols != b->cols || a->cols < 1 || !row_dtype(dtype) || ldo < b->rows) return STX_ERR_BAD_ARG;
     if (a->rows == 0 || b->rows == 0) return STX_OK;
-    if (a->ld > ((int64_t)1 << 24) || b->ld > ((int64_t)1 << 24)) return STX_ERR_UNSUPPORTED;   // a tile's rows: 32-bit offsets
+    for (const stx_q8 *q : {a, b})         // a tile's rows: 32-bit offsets
+        if (q->ld > ((int64_t)1 << 24) || q->ld_scale > ((int64_t)1 << 24)) return STX_ERR_UNSUPPORTED;
     if (a->rows > ((int64_t)1 << 44) / b->rows) return STX_ERR_UNSUPPORTED;                       // tiles of one launch
     if (!out) return STX_ERR_NULL;
     if (!aligned(out, element(dtype))) return STX_ERR_BAD_ARG;

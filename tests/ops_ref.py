@@ -5,7 +5,7 @@ import numpy as np
 import torch
 
 U = 2.0**-24                               # half a step of fp32, relative
-HALF = {torch.float32: U, torch.bfloat16: 2.0**-9, torch.float16: 2.0**-12}   # at most half a step, relative to the value
+HALF = {torch.float32: U, torch.bfloat16: 2.0**-8, torch.float16: 2.0**-11}   # at most half a step, relative to the value
 BLOCK = 128
 FORMATS = {0: (torch.float8_e4m3fn, 3, -6, 448.0), 1: (torch.float8_e5m2, 2, -14, 57344.0)}
 

@@ -120,7 +120,7 @@ def check_product(got, x, y, dtype, cols):
     them.  16 bits: in every eight products up to seven are cut below 2^-13 of the eight's largest.  Then one rounding."""
     want, total = x @ y.T, np.abs(x) @ np.abs(y).T
     nb = -(-cols // 128)
-    tol = (4 * 4 * nb + 16) * 2.0**-23 * total + 2 * R.HALF[dtype] * np.abs(want) + (2.0**-25 if dtype == torch.float16 else 0)
+    tol = (4 * 4 * nb + 16) * 2.0**-23 * total + R.HALF[dtype] * np.abs(want) + (2.0**-25 if dtype == torch.float16 else 0)
     if dtype != torch.float32:
         tol += 7 * 2.0**-13 * total
     err = np.abs(R.f64(got) - want)

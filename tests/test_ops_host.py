@@ -112,9 +112,10 @@ def test_quantize_refusals(kw, status):
     (dict(out=None), B.STX_ERR_NULL),
     (dict(out=P + 2), B.STX_ERR_BAD_ARG),
     (dict(a=q8(ld=(1 << 24) + 16)), B.STX_ERR_UNSUPPORTED),
+    (dict(b=q8(ld_scale=(1 << 24) + 4)), B.STX_ERR_UNSUPPORTED),
     (dict(a=q8(rows=1 << 30), b=q8(rows=1 << 30), ldo=1 << 30), B.STX_ERR_UNSUPPORTED),
-    (dict(a=q8(cols=100_000, ld=100_096, ld_scale=784), b=q8(cols=100_000, ld=100_096, ld_scale=784), work=None), B.STX_ERR_NULL),
-    (dict(a=q8(cols=100_000, ld=100_096, ld_scale=784), b=q8(cols=100_000, ld=100_096, ld_scale=784), work_bytes=4), B.STX_ERR_WORKSPACE),
+    (dict(a=q8(rows=40, cols=100_000, ld=100_096, ld_scale=784), b=q8(rows=40, cols=100_000, ld=100_096, ld_scale=784), ldo=40, work=None), B.STX_ERR_NULL),
+    (dict(a=q8(rows=40, cols=100_000, ld=100_096, ld_scale=784), b=q8(rows=40, cols=100_000, ld=100_096, ld_scale=784), ldo=40, work_bytes=4), B.STX_ERR_WORKSPACE),
 ])
 def test_matmul_refusals(kw, status):
     a = dict(ctx=context(), a=q8(), b=q8(), dtype=B.STX_F32, out=P, ldo=4, work=P, work_bytes=1 << 30)
@@ -141,7 +142,7 @@ def hyper(**kw):
     return B.make_adamw(**a)
 
 
-BAD_HYPER = [dict(bits=16), dict(lr=float("nan")), dict(beta1=1.0), dict(beta2=-0.1), dict(beta2=float("nan")), dict(eps=-1.0), dict(step=0),
+BAD_HYPER = [dict(bits=16), dict(lr=float("nan")), dict(beta1=1.0), dict(beta2=-0.1), dict(beta2=float("nan")), dict(eps=-1.0), dict(eps=1e-40), dict(eps=1e39), dict(step=0),
              dict(weight_decay=float("nan"))]
 
 
