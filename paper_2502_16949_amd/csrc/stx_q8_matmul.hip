@@ -77,13 +77,13 @@ __device__ inline void store4(const MmArgs &p, int split, int64_t i, int64_t j, 
         for (int r = 0; r < 4 && j + r < p.n; ++r) o[r] = h[r];
 }
 
-// The workgroup's tile: every die takes a run of consecutive tiles (workgroups go round the dies in turn), along stripes of
+// Tile number `number`: every die takes a run of consecutive tiles (workgroups go round the dies in turn), along stripes of
 // kStripe tiles of A, so that what a die reads at a time fits its L2.
 constexpr int kDies = 8, kStripe = 8;
-__device__ inline void tile_of(const MmArgs &p, int &tm, int &tn, int &split)
+__device__ inline void tile_of(const MmArgs &p, unsigned number, unsigned total, int &tm, int &tn, int &split)
 {
-    const unsigned total = gridDim.x, die = blockIdx.x % kDies, each = total / kDies, more = total % kDies;
-    const unsigned i = die * each + (die < more ? die : more) + blockIdx.x / kDies;
+    const unsigned die = number % kDies, each = total / kDies, more = total % kDies;
+    const unsigned i = die * each + (die < more ? die : more) + number / kDies;
     const unsigned tiles = (unsigned)p.ntm * (unsigned)p.ntn;
     split = __builtin_amdgcn_readfirstlane((int)(i / tiles));
     const unsigned t = i % tiles, stripe = t / (unsigned)(kStripe * p.ntn), r = t % (unsigned)(kStripe * p.ntn);
@@ -210,19 +210,28 @@ __device__ inline void store_piece(T *out, const MmArgs &p, int split, int64_t i
         if (j + r < p.n) o[r] = v[r];
 }
 
+// Between LDS accesses of all wavefronts; stores stay under way.
+__device__ inline void leave_sync()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 // A workgroup's outputs turn in LDS, so that its rows leave whole: as they stand, a store would have 16 bytes of 32 rows.  PASSES
-// parts of a wavefront's rows after each other (fp32: room).  Pieces of 16 bytes are permuted by the row.  All wavefronts call it,
-// when nothing else of the LDS is in use.
+// parts of a wavefront's rows after each other, so many as NW * 8 KB need.  Pieces of 16 bytes are permuted by the row.  All
+// wavefronts call it, when nothing else of that LDS is in use; their own requests have arrived before the first store, which a
+// wait for them would wait for too.
 template <class T, bool PAST, int BM, int BN, int WM, int WN, int MI, int NI>
 __device__ inline void leave_as(const MmArgs &p, int split, int64_t m0, int64_t n0, const f32x16_t (&acc)[MI][NI], uint8_t *lds)
 {
-    constexpr int PASSES = sizeof(T) / 2, ROWS = BM / PASSES, PART = MI / PASSES, LINE = BN * sizeof(T), PIECES = LINE / 16;
+    constexpr int PASSES = BM * BN * sizeof(T) / (WM * WN * 8192), ROWS = BM / PASSES, PART = MI / PASSES, LINE = BN * sizeof(T), PIECES = LINE / 16;
     constexpr int PER = 1024 / LINE, NW = WM * WN;           // rows of a wavefront's store
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l31 = lane & 31, half = lane >> 5;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));         // (no address of these is kept through the products)
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l31 = lane & 31, half = lane >> 5;
     const int wm = wave % WM, wn = wave / WM * (BN / WN);
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
-        __syncthreads();
+        if (pass) leave_sync();
 #pragma unroll
         for (int i = 0; i < PART; ++i) {
             uint8_t *line = lds + ((wm * PART + i) * 32 + l31) * LINE;
@@ -244,7 +253,8 @@ __device__ inline void leave_as(const MmArgs &p, int split, int64_t m0, int64_t 
                     }
                 }
         }
-        __syncthreads();
+        if (pass == 0) __builtin_amdgcn_s_waitcnt(0x0f70);
+        leave_sync();
 #pragma unroll 4
         for (int it = 0; it < ROWS / (NW * PER); ++it) {
             const int lr = (it * NW + wave) * PER + lane / PIECES, c = (lane % PIECES) ^ (lr & 15);
@@ -255,10 +265,10 @@ __device__ inline void leave_as(const MmArgs &p, int split, int64_t m0, int64_t 
         }
     }
 }
-template <int BM, int BN, int WM, int WN, int MI, int NI>
+template <bool WIDE, int BM, int BN, int WM, int WN, int MI, int NI>
 __device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0, const f32x16_t (&acc)[MI][NI], uint8_t *lds)
 {
-    if (p.dtype == STX_F32) {
+    if (WIDE || p.dtype == STX_F32) {
         if (p.past) leave_as<float, true, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
         else leave_as<float, false, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
     } else if (p.dtype == STX_BF16) {
@@ -284,33 +294,49 @@ __device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0,
 //
 // (of stage s; group 1 still multiplies s - 1 in phase 4s).  A stage's codes of A are requested beside the first reads of the stage before,
 // when everybody has read their buffer, those of B, which only one group reads, between that group's products two stages before.
-// (All of them beside the reads made those phases the longest: 8,192 x 8,192 x 8,192 in 460 us.)  Every wavefront waits for its own
+// (All of them beside the reads made those phases the longest: 8,192 x 8,192 x 8,192 in 460 us, so in 438.)  Every wavefront waits for its own
 // at the end of 4s + 3, before the first read of the next stage; group 0 leaves those in flight that it has just requested.
+//
+// One workgroup for each compute unit takes every 256th tile, and requests the next one's first stage before its outputs leave (4,096 x
+// 14,951 bf16 over 1,024 columns in 85 us, with a workgroup for each tile in 91).
 template <int BM, int BN, int WM, int WN, bool WIDE, int FA, int FB>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
 {
     constexpr int NW = WM * WN, MI = BM / WM / 32, NI = BN / WN / 32, LA = BM / 8 / NW, LB = BN / 8 / NW, BUF = (BM + BN) * kBlock;
     constexpr bool PHASES = NW == 8;
-    static_assert(BM + BN <= NW * 64 && 2 * BUF >= NW * MI * 4096, "a thread for each row's scales; room for the outputs");
-    __shared__ __align__(16) uint8_t s_buf[2 * BUF];
+    constexpr int ROOM = NW * 8192;        // what the outputs turn in, from the second buffer on
+    static_assert(BM + BN <= NW * 64, "a thread for each row's scales");
+    __shared__ __align__(16) uint8_t s_buf[BUF + (BUF > ROOM ? BUF : ROOM)];
     __shared__ uint32_t s_scale[2][BM + BN];                 // a word for four stages
-    int tm, tn, split;
-    tile_of(p, tm, tn, split);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int l31 = lane & 31, half = lane >> 5, group = wave >> 2;
-    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-    const int kb0 = split * p.kb_split, stages = min(kb0 + p.kb_split, p.nkb) - kb0;
     // requests: a wavefront's 64 pieces are 8 rows, of B the rows that its group reads; rows behind the last one repeat it.  Offsets of
     // 32 bits to a scalar base: a 64-bit sum in a vector register would wait until the other group's products are done
     const int piece = ((lane & 7) ^ ((wave * 4 + (lane >> 4)) & 7)) * 16;
     constexpr int NG = PHASES ? 4 : NW;    // wavefronts of a group
     const int b_first = PHASES ? group * (BN / 16) + (wave & 3) : wave;         // in eights of rows
-    uint32_t oa[LA], ob[LB];
+    const bool of_a = wave * 64 < BM;      // whose rows' scales this wavefront requests
+    uint32_t oa[LA], ob[LB], os;
+    const uint8_t *ga, *gb, *gs;
+    int64_t m0, n0;
+    int split, stages;
+    auto aim = [&](unsigned number, unsigned total) {
+        int tm, tn, l8 = lane >> 3, thread = threadIdx.x;
+        asm volatile("" : "+v"(l8), "+v"(thread));
+        tile_of(p, number, total, tm, tn, split);
+        m0 = (int64_t)tm * BM;
+        n0 = (int64_t)tn * BN;
+        const int kb0 = split * p.kb_split;
+        stages = min(kb0 + p.kb_split, p.nkb) - kb0;
 #pragma unroll
-    for (int i = 0; i < LA; ++i) oa[i] = (uint32_t)(min((int64_t)((i * NW + wave) * 8 + (lane >> 3)), p.m - 1 - m0) * p.lda) + piece;
+        for (int i = 0; i < LA; ++i) oa[i] = (uint32_t)(min((int64_t)((i * NW + wave) * 8 + l8), p.m - 1 - m0) * p.lda) + piece;
 #pragma unroll
-    for (int i = 0; i < LB; ++i) ob[i] = (uint32_t)(min((int64_t)((i * NG + b_first) * 8 + (lane >> 3)), p.n - 1 - n0) * p.ldb) + piece;
-    const uint8_t *ga = p.a + m0 * p.lda + (int64_t)kb0 * kBlock, *gb = p.b + n0 * p.ldb + (int64_t)kb0 * kBlock;
+        for (int i = 0; i < LB; ++i) ob[i] = (uint32_t)(min((int64_t)((i * NG + b_first) * 8 + l8), p.n - 1 - n0) * p.ldb) + piece;
+        ga = p.a + m0 * p.lda + (int64_t)kb0 * kBlock;
+        gb = p.b + n0 * p.ldb + (int64_t)kb0 * kBlock;
+        gs = (of_a ? p.as + m0 * p.ldas : p.bs + n0 * p.ldbs) + kb0;
+        os = of_a ? (uint32_t)(min((int64_t)thread, p.m - 1 - m0) * p.ldas) : (uint32_t)(min((int64_t)thread - BM, p.n - 1 - n0) * p.ldbs);
+    };
     auto request = [&](const uint8_t *from, uint32_t &at, uint8_t *to) {
         asm volatile("" : "+v"(at));       // (keeps it 32 bits)
         __builtin_amdgcn_global_load_lds((global_ptr_t)(from + at), (lds_ptr_t)to, 16, 0, 0);
@@ -321,10 +347,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
         ga += kBlock;
     };
     auto fetch_b = [&](int buf, int i) { request(gb, ob[i], s_buf + buf * BUF + BM * kBlock + (i * NG + b_first) * 1024); };
-    const bool of_a = wave * 64 < BM;      // whose rows' scales this wavefront requests
-    const uint8_t *gs = (of_a ? p.as + m0 * p.ldas : p.bs + n0 * p.ldbs) + kb0;
-    uint32_t os = of_a ? (uint32_t)(min((int64_t)threadIdx.x, p.m - 1 - m0) * p.ldas)
-                             : (uint32_t)(min((int64_t)threadIdx.x - BM, p.n - 1 - n0) * p.ldbs);
     auto fetch_scales = [&](int to) {
         if (wave * 64 >= BM + BN) return;
         asm volatile("" : "+v"(os));
@@ -338,12 +360,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
     const uint32_t lds_scale = (uint32_t)(uintptr_t)(lds_ptr_t)&s_scale[0][0];
     const uint32_t at_sa = lds_scale + 4 * (wm + l31), at_sb = lds_scale + 4 * (BM + wn + l31);
     f32x16_t acc[MI][NI];
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     uint32_t sca[MI], scb[NI];
     i32x4_t a[MI][2], b[NI][2];
     uint32_t fa = 0, fb = 0;
@@ -364,46 +380,68 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
         for (int i = 0; i < LB; ++i) fetch_b(s & 1, i);
         if (s + 1 < stages) gb += kBlock;
     };
+    const unsigned total = (unsigned)p.ntm * (unsigned)p.ntn * (unsigned)p.splits;
+    aim(blockIdx.x, total);
     fetch_scales(0);
     fetch_a(0);
     all_b(0);
-    if constexpr (PHASES) {
-        all_b(1);
-        __builtin_amdgcn_s_waitcnt(0x0f70 + LB);             // vmcnt(LB): all but stage 1's
+    for (unsigned number = blockIdx.x; ; number += gridDim.x) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        if constexpr (PHASES) {
+            all_b(1);
+            if (number == blockIdx.x) __builtin_amdgcn_s_waitcnt(0x0f70 + LB);  // vmcnt(LB): all but stage 1's
+            phase_end();
+            if (group == 1) phase_end();
+        }
+        for (int s = 0; s < stages; ++s) {
+            if constexpr (!PHASES) {
+                __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0)
+                phase_end();
+            }
+            if ((s & 3) == 0 && s + 4 < stages) fetch_scales(((s >> 2) + 1) & 1);
+            if (s + 1 < stages) fetch_a((s + 1) & 1);
+            if (!PHASES && s + 1 < stages) all_b(s + 1);
+            read_first(s);
+            if constexpr (PHASES) phase_end();
+            multiply([](int) {});
+            if constexpr (PHASES) phase_end();
+            read_step(fa ^ 64u, fa ^ 96u, fb ^ 64u, fb ^ 96u, a, b);
+            if constexpr (!PHASES) multiply([](int) {});
+            else {
+                if (group == 1) __builtin_amdgcn_s_waitcnt(0x0f70);
+                phase_end();
+                multiply([&](int u) {
+                    if (u % 2) return;
+                    keep_order();
+                    fetch_b(s & 1, u / 2);
+                    keep_order();
+                });
+                if (s + 3 < stages) gb += kBlock;
+                if (group == 0) __builtin_amdgcn_s_waitcnt(0x0f70 + LB);
+                phase_end();
+            }
+        }
+        if (PHASES && group == 0) phase_end();
+        __builtin_amdgcn_s_waitcnt(0x0f70);
         phase_end();
-        if (group == 1) phase_end();
-    }
-    for (int s = 0; s < stages; ++s) {
-        if constexpr (!PHASES) {
-            __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0)
-            phase_end();
+        const int64_t m_out = m0, n_out = n0;
+        const int split_out = split;
+        const bool more = PHASES && number + gridDim.x < total;
+        if (more) {                        // the next tile's first stage
+            aim(number + gridDim.x, total);
+            fetch_scales(0);
+            fetch_a(0);
+            all_b(0);
         }
-        if ((s & 3) == 0 && s + 4 < stages) fetch_scales(((s >> 2) + 1) & 1);
-        if (s + 1 < stages) fetch_a((s + 1) & 1);
-        if (!PHASES && s + 1 < stages) all_b(s + 1);
-        read_first(s);
-        if constexpr (PHASES) phase_end();
-        multiply([](int) {});
-        if constexpr (PHASES) phase_end();
-        read_step(fa ^ 64u, fa ^ 96u, fb ^ 64u, fb ^ 96u, a, b);
-        if constexpr (!PHASES) multiply([](int) {});
-        else {
-            if (group == 1) __builtin_amdgcn_s_waitcnt(0x0f70);
-            phase_end();
-            multiply([&](int u) {
-                if (u % 2) return;
-                keep_order();
-                fetch_b(s & 1, u / 2);
-                keep_order();
-            });
-            if (s + 3 < stages) gb += kBlock;
-            if (group == 0) __builtin_amdgcn_s_waitcnt(0x0f70 + LB);
-            phase_end();
-        }
+        leave<WIDE, BM, BN, WM, WN>(p, split_out, m_out, n_out, acc, s_buf + BUF);
+        if (!more) break;
+        phase_end();
     }
-    if (PHASES && group == 0) phase_end();
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-    leave<BM, BN, WM, WN>(p, split, m0, n0, acc, s_buf);
 }
 
 // The slices' sums, joined in order.
@@ -590,7 +628,8 @@ static void mm_go(stx_ctx *c, const MmPlan &t, bool wide, const MmArgs &p)
 #undef STX_DIRECT
         return;
     }
-    const dim3 grid((unsigned)(t.ntm * t.ntn * t.splits));
+    const int64_t tiles = t.ntm * t.ntn * t.splits;
+    const dim3 grid((unsigned)(t.bm == 128 ? tiles : tiles < 256 ? tiles : 256));
     ProfScope prof(c, "k_q8_mm");
     if (t.bm != t.bn) {
         hipLaunchKernelGGL((k_q8_mm<256, 128, 4, 2, true, FA, FB>), grid, dim3(512), 0, c->stream, p);
@@ -609,12 +648,12 @@ stx_status launch_q8_matmul(stx_ctx *c, const stx_q8 *a, const stx_q8 *b, int dt
     const MmPlan t = mm_plan(a->rows, b->rows, a->cols, wide);
     MmArgs p{a->codes, a->scales, b->codes, b->scales, a->ld, a->ld_scale, b->ld, b->ld_scale, a->rows, b->rows,
              (int)((a->cols + kBlock - 1) / kBlock), t.kb_split, t.splits, (int)t.ntm, (int)t.ntn, out, ldo, dtype, 0};
-    // Outputs beyond the caches go past them, 4,096 x 14,848 bf16 over 1,024 columns in 79 us in place of 105.  Rows that are not
-    // whole lines leave parts of lines, which meet in the caches only where tiles are short (4,096 x 14,951: over 1,024 columns 93 us
-    // past the caches and 98 through them, over 128 columns 51 and 48).
+    // Outputs beyond the caches go past them: 16,384 x 40,448 bf16 over 256 columns in 356 us in place of 452, over 1,024 (40,559)
+    // 748 in place of 924.  Rows that are not whole lines leave parts of lines, which meet in the caches only where tiles are short
+    // (4,096 x 14,951: over 128 columns 51 us past the caches and 43 through them; over 256, by 40,559, 520 and 560; over 512 63 and 66).
     const int64_t size = dtype == STX_F32 ? 4 : 2;
     const bool lines = ldo * size % 128 == 0 && (uintptr_t)out % 128 == 0;
-    p.past = t.splits == 1 && p.m * p.n * size >= ((int64_t)64 << 20) && (lines || p.nkb >= 8);
+    p.past = t.splits == 1 && p.m * p.n * size >= ((int64_t)64 << 20) && (lines || p.nkb >= 2);
     if (t.splits > 1) {
         p.out = work;
         p.ldo = p.n;
