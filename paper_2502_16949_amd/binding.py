@@ -415,7 +415,10 @@ class Q8:
             assert t.is_cuda and t.dtype == torch.uint8 and t.dim() == 2 and t.stride(1) == 1 and t.shape[0] == codes.shape[0]
         assert codes.shape[1] >= (cols + 127) // 128 * 128 and scales.shape[1] >= (cols + 127) // 128
         self.codes, self.scales, self.rows, self.cols, self.format = codes, scales, codes.shape[0], cols, format
+        self.index = codes.get_device()
+        assert scales.get_device() == self.index
         self.c = stx_q8(_ptr(codes), _ptr(scales), codes.shape[0], cols, codes.stride(0), scales.stride(0), format)
+        self.ref = C.byref(self.c)
 
 
 def _rows2d(ctx, first, *others):
@@ -446,8 +449,10 @@ def _work(ctx, work):
 
 
 def _q8(ctx, q):
-    assert q is None or q.codes.get_device() == q.scales.get_device() == ctx.index
-    return None if q is None else C.byref(q.c)
+    if q is None:
+        return None
+    assert q.index == ctx.index
+    return q.ref
 
 
 def stx_rmsnorm(ctx: Context, x, residual, weight, eps: float, sum, y, q, rstd):
