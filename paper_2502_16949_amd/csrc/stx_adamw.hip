@@ -18,8 +18,11 @@
 
 namespace stx {
 
-constexpr int kAdamTensors = 48;           // tensors of one launch: their descriptions travel as kernel arguments (4 KB)
-constexpr int kAdamOctets = 2;             // octets of a thread: a workgroup takes 4,096 elements
+// Tensors of one launch: their descriptions travel as kernel arguments.  4 KB of them, or, for up to 8 tensors, 0.8 KB
+// (a call on 6 small ones takes the host 10.4 us with 4 KB, so 9.5).
+constexpr int kAdamTensors = 48, kAdamFew = 8;
+// Octets of a thread: a workgroup takes 4,096 elements (one octet: 4,000,000 x 128 in 8 bits in 1,344 us, two: 1,320).
+constexpr int kAdamOctets = 2;
 constexpr int kAdamTile = kThreads * 8 * kAdamOctets;
 
 struct AdamCoef {
@@ -45,10 +48,11 @@ struct AdamTensorArg {
     uint32_t first;                        // first workgroup of the tensor
     uint16_t g_dtype, flags;
 };
+template <int N>
 struct AdamTensorsArgs {
     AdamHyper h;
     int n, first_tensor;
-    AdamTensorArg t[kAdamTensors];
+    AdamTensorArg t[N];
 };
 
 // b^t by squaring, in double: the same on the host and here.
@@ -178,8 +182,8 @@ __device__ inline void load_grads(const AdamTensorArg &t, int64_t blk0, int l16,
         }
 }
 
-template <int BITS>
-__global__ __launch_bounds__(kThreads) void k_adamw_tensors(AdamTensorsArgs a)
+template <int BITS, int N>
+__global__ __launch_bounds__(kThreads) void k_adamw_tensors(AdamTensorsArgs<N> a)
 {
     // the tensor of this workgroup: the last one whose first workgroup is not behind it
     const int lane = threadIdx.x & 63;
@@ -506,29 +510,36 @@ static AdamHyper make_hyper(const stx_adamw *h)
     return a;
 }
 
-stx_status launch_adamw_tensors(stx_ctx *c, const stx_adamw *h, const stx_adamw_tensor *tensors, int n)
+// Tensors from number i on, as many as one launch takes; false: all of them empty.
+template <int N>
+static bool adam_tensors_go(stx_ctx *c, const stx_adamw *h, const stx_adamw_tensor *tensors, int n, int &i)
 {
-    AdamTensorsArgs a{};
+    AdamTensorsArgs<N> a;
     static_assert(sizeof(a) <= 4096, "kernel arguments");
     a.h = make_hyper(h);
+    a.n = 0;
+    a.first_tensor = i;
+    uint64_t blocks = 0;
+    for (; i < n && a.n < N; ++i) {
+        const stx_adamw_tensor &t = tensors[i];
+        const uint64_t need = ((uint64_t)t.n + kAdamTile - 1) / kAdamTile;
+        if (blocks + need > 0x7fffffffull) break;            // (the host has checked that one tensor fits)
+        // (an empty tensor shares its first workgroup with the next one, which the search finds)
+        a.t[a.n++] = {t.p, t.g, t.s.m, t.s.v, t.s.m_scale, t.s.v_scale, t.n, (uint32_t)blocks, (uint16_t)t.g_dtype, (uint16_t)t.flags};
+        blocks += need;
+    }
+    if (!blocks) return false;
+    ProfScope prof(c, "k_adamw_tensors");
+    if (h->bits == 8) hipLaunchKernelGGL((k_adamw_tensors<8, N>), dim3((unsigned)blocks), dim3(kThreads), 0, c->stream, a);
+    else hipLaunchKernelGGL((k_adamw_tensors<32, N>), dim3((unsigned)blocks), dim3(kThreads), 0, c->stream, a);
+    return true;
+}
+
+stx_status launch_adamw_tensors(stx_ctx *c, const stx_adamw *h, const stx_adamw_tensor *tensors, int n)
+{
     bool launched = false;
     for (int i = 0; i < n;) {
-        uint64_t blocks = 0;
-        a.n = 0;
-        a.first_tensor = i;
-        for (; i < n && a.n < kAdamTensors; ++i) {
-            const stx_adamw_tensor &t = tensors[i];
-            const uint64_t need = ((uint64_t)t.n + kAdamTile - 1) / kAdamTile;
-            if (blocks + need > 0x7fffffffull) break;        // (the host has checked that one tensor fits)
-            // (an empty tensor shares its first workgroup with the next one, which the search finds)
-            a.t[a.n++] = {t.p, t.g, t.s.m, t.s.v, t.s.m_scale, t.s.v_scale, t.n, (uint32_t)blocks, (uint16_t)t.g_dtype, (uint16_t)t.flags};
-            blocks += need;
-        }
-        if (!blocks) continue;
-        launched = true;
-        ProfScope prof(c, "k_adamw_tensors");
-        if (h->bits == 8) hipLaunchKernelGGL(k_adamw_tensors<8>, dim3((unsigned)blocks), dim3(kThreads), 0, c->stream, a);
-        else hipLaunchKernelGGL(k_adamw_tensors<32>, dim3((unsigned)blocks), dim3(kThreads), 0, c->stream, a);
+        if (n <= kAdamFew ? adam_tensors_go<kAdamFew>(c, h, tensors, n, i) : adam_tensors_go<kAdamTensors>(c, h, tensors, n, i)) launched = true;
     }
     return launched ? hip_ok(hipGetLastError()) : STX_OK;
 }
