@@ -84,32 +84,36 @@ __device__ inline Octet<T> request_octet(const T *row, int blk, int l16, int64_t
     }
     return o;
 }
-// N elements moved down by `by` places of 0 to N, zeros behind them.
-template <int N>
-__device__ inline void shift_down(float *v, int by)
+// Puts the elements of request_octet(row, blk, l16, n) into place; 0 behind the row's end.
+template <class T>
+__device__ inline void settle_octet(Octet<T> &o, int blk, int l16, int64_t n)
 {
+    constexpr int N = 16 / sizeof(T);      // elements of an access
+    if (n < N || !__ballot(octet_pos<T>(blk, l16, 8 - N) + N > n)) return;
 #pragma unroll
-    for (int s = N; s >= 1; s >>= 1)
+    for (int h = 0; h < 8 / N; ++h) {
+        const int64_t over = octet_pos<T>(blk, l16, h * N) + N - n;
+        const int by = (int)(over < 0 ? 0 : over > N ? N : over);
+        uint32_t *w = o.w + 4 * h;
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = (by & s) ? (j + s < N ? v[j + s] : 0.f) : v[j];
+        for (int u = 4; u >= 1; u >>= 1)   // whole words down
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = (by * (int)sizeof(T) / 4 & u) ? (j + u < 4 ? w[j + u] : 0u) : w[j];
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = (by & 1) ? w[j] >> 16 | (j < 3 ? w[j + 1] << 16 : 0u) : w[j];
+        }
+    }
 }
 // The elements of request_octet(row, blk, l16, n) as floats; 0 behind the row's end.
 template <class T>
-__device__ inline void octet_floats(const Octet<T> &o, int blk, int l16, int64_t n, float (&v)[8])
+__device__ inline void octet_floats(Octet<T> o, int blk, int l16, int64_t n, float (&v)[8])
 {
-    constexpr int N = 16 / sizeof(T);
+    settle_octet(o, blk, l16, n);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         if constexpr (sizeof(T) == 4) v[j] = __builtin_bit_cast(float, o.w[j]);
         else v[j] = to_float<T>((uint16_t)(o.w[j / 2] >> (16 * (j & 1))));
-    }
-    const int64_t last = octet_pos<T>(blk, l16, 8 - N);
-    if (n >= N && __ballot(last + N > n)) {
-#pragma unroll
-        for (int h = 0; h < 8 / N; ++h) {
-            const int64_t over = octet_pos<T>(blk, l16, h * N) + N - n;
-            shift_down<N>(v + h * N, (int)(over < 0 ? 0 : over > N ? N : over));
-        }
     }
 }
 
@@ -183,6 +187,58 @@ constexpr uint32_t kInfBits = 0x7f800000u;
 __device__ inline uint32_t abs_bits(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
 __device__ inline uint32_t finite_bits(float v) { const uint32_t b = abs_bits(v); return b < kInfBits ? b : 0u; }
 
+// Largest finite magnitudes, as bits of an fp32: over N numbers, and over N pairs of 16-bit numbers, of each half.  What is not
+// finite is left out in a second pass, by wavefronts that have met one.
+template <int N>
+__device__ inline uint32_t largest(const float *v)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) m = max(m, abs_bits(v[j]));
+    if (__ballot(m >= kInfBits)) {
+        m = 0;
+#pragma unroll
+        for (int j = 0; j < N; ++j) m = max(m, finite_bits(v[j]));
+    }
+    return m;
+}
+template <class T, int N>
+__device__ inline void largest_pair(const uint32_t *w, uint32_t &lo, uint32_t &hi)
+{
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+    constexpr uint32_t inf = __is_same(T, bf16_t) ? 0x7f80u : 0x7c00u;
+    u16x2_t m = {0, 0};
+#pragma unroll
+    for (int j = 0; j < N; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2_t, w[j] & 0x7fff7fffu));
+    lo = m.x;
+    hi = m.y;
+    if (__ballot(max(lo, hi) >= inf)) {
+        lo = hi = 0;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const uint32_t a = w[j] & 0x7fffu, b = w[j] >> 16 & 0x7fffu;
+            lo = max(lo, a < inf ? a : 0u);
+            hi = max(hi, b < inf ? b : 0u);
+        }
+    }
+    lo = __builtin_bit_cast(uint32_t, to_float<T>((uint16_t)lo));
+    hi = __builtin_bit_cast(uint32_t, to_float<T>((uint16_t)hi));
+}
+template <class T>
+__device__ inline uint32_t largest(const Octet<T> &o)
+{
+    if constexpr (sizeof(T) == 4) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __builtin_bit_cast(float, o.w[j]);
+        return largest<8>(v);
+    } else {
+        uint32_t lo, hi;
+        largest_pair<T, 4>(o.w, lo, hi);
+        return max(lo, hi);
+    }
+}
+
 // The exponent byte of a block's scale from the bits of its largest finite magnitude: both formats' largest numbers are 1.75
 // times a power of two, so a magnitude 1.f 2^E needs 2^(E - 8), or one power more where 1.f > 1.75.
 template <int FORMAT>
@@ -192,8 +248,7 @@ __device__ inline uint32_t block_scale(uint32_t most)
     const int e = (int)(most >> 23) - top + ((most & 0x7fffffu) > 0x600000u ? 1 : 0);   // biased by 127 like fp32's
     return most == 0u ? 127u : (uint32_t)max(e, 1);
 }
-// 2^-(byte - 127); byte 1..254
-__device__ inline float scale_down(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }
+__device__ inline float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // Four numbers as codes, nearest even; what lies above the format's largest number by less than half a step rounds to it.
 template <int FORMAT>
@@ -223,12 +278,58 @@ __device__ inline void unpack4(uint32_t w, float *v)
     }
     v[0] = lo.x; v[1] = lo.y; v[2] = hi.x; v[3] = hi.y;
 }
-// A number scaled for its code; an infinity, which E4M3 has not, becomes a NaN.
+// Two numbers over a power of two as codes, nearest even, into the low or the high half of `codes`.  NaN stays NaN; infinities stay
+// in E5M2 and become NaN in E4M3.  (These instructions agree with a product and v_cvt_pk_* in every 16-bit number and scale.)
+typedef int16_t i16x2_t __attribute__((ext_vector_type(2)));
 template <int FORMAT>
-__device__ inline float scaled(float v, float down)
+__device__ inline i16x2_t code2(i16x2_t codes, float a, float b, float scale, bool high)
 {
-    if constexpr (FORMAT == STX_E4M3) return abs_bits(v) < kInfBits ? v * down : __builtin_bit_cast(float, 0x7fc00000u);
-    return v * down;
+    if constexpr (FORMAT == STX_E4M3)
+        return high ? __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(codes, a, b, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(codes, a, b, scale, false);
+    else
+        return high ? __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(codes, a, b, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(codes, a, b, scale, false);
+}
+template <class T, int FORMAT>
+__device__ inline i16x2_t code2(i16x2_t codes, uint32_t pair, float scale, bool high)
+{
+    if constexpr (__is_same(T, bf16_t)) {
+        typedef __bf16 v2_t __attribute__((ext_vector_type(2)));
+        const v2_t v = __builtin_bit_cast(v2_t, pair);
+        if constexpr (FORMAT == STX_E4M3)
+            return high ? __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(codes, v, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(codes, v, scale, false);
+        else
+            return high ? __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(codes, v, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(codes, v, scale, false);
+    } else {
+        typedef _Float16 v2_t __attribute__((ext_vector_type(2)));
+        const v2_t v = __builtin_bit_cast(v2_t, pair);
+        if constexpr (FORMAT == STX_E4M3)
+            return high ? __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(codes, v, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(codes, v, scale, false);
+        else
+            return high ? __builtin_amdgcn_cvt_scalef32_pk_bf8_f16(codes, v, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf8_f16(codes, v, scale, false);
+    }
+}
+template <int FORMAT>
+__device__ inline uint32_t code4(float a, float b, float c, float d, float scale)
+{
+    return __builtin_bit_cast(uint32_t, code2<FORMAT>(code2<FORMAT>(i16x2_t{0, 0}, a, b, scale, false), c, d, scale, true));
+}
+template <class T, int FORMAT>
+__device__ inline uint32_t code4(uint32_t ab, uint32_t cd, float scale)
+{
+    return __builtin_bit_cast(uint32_t, code2<T, FORMAT>(code2<T, FORMAT>(i16x2_t{0, 0}, ab, scale, false), cd, scale, true));
+}
+// The codes of an octet.
+template <class T, int FORMAT>
+__device__ inline uint2 code8(const Octet<T> &o, float scale)
+{
+    if constexpr (sizeof(T) == 4) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __builtin_bit_cast(float, o.w[j]);
+        return make_uint2(code4<FORMAT>(v[0], v[1], v[2], v[3], scale), code4<FORMAT>(v[4], v[5], v[6], v[7], scale));
+    } else {
+        return make_uint2(code4<T, FORMAT>(o.w[0], o.w[1], scale), code4<T, FORMAT>(o.w[2], o.w[3], scale));
+    }
 }
 
 // A kernel's view of an stx_q8 that it writes (codes null: none).
@@ -237,28 +338,33 @@ struct Q8Out {
     int64_t ld, ld_scale;
 };
 
-// An octet's codes and, by the block's first lane, its scale.  All 16 lanes of the block call it; elements behind the last
-// column are 0 and get codes of 0.
+// An octet's codes and, by the block's first lane, its scale.
+template <class T>
+__device__ inline void store_codes(const Q8Out &q, int64_t row, int blk, int l16, uint2 codes, uint32_t byte)
+{
+    uint8_t *at = q.codes + row * q.ld + blk * kBlock;
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<uint32_t *>(at + 4 * l16) = codes.x;
+        *reinterpret_cast<uint32_t *>(at + 64 + 4 * l16) = codes.y;
+    } else {
+        *reinterpret_cast<uint2 *>(at + 8 * l16) = codes;
+    }
+    if (l16 == 0) q.scales[row * q.ld_scale + blk] = (uint8_t)byte;
+}
+// Of an octet, as it lies in memory or (with the layout of T) as floats.  All 16 lanes of the block call it; elements behind the
+// last column are 0 and get codes of 0.
+template <class T, int FORMAT>
+__device__ inline void store_q8_octet(const Q8Out &q, int64_t row, int blk, int l16, const Octet<T> &o)
+{
+    const uint32_t byte = block_scale<FORMAT>(row16_max(largest(o)));
+    store_codes<T>(q, row, blk, l16, code8<T, FORMAT>(o, scale_of(byte)), byte);
+}
 template <class T, int FORMAT>
 __device__ inline void store_q8_octet(const Q8Out &q, int64_t row, int blk, int l16, const float (&v)[8])
 {
-    uint32_t most = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) most = max(most, finite_bits(v[j]));
-    const uint32_t byte = block_scale<FORMAT>(row16_max(most));
-    const float down = scale_down(byte);
-    float s[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = scaled<FORMAT>(v[j], down);
-    const uint32_t lo = pack4<FORMAT>(s[0], s[1], s[2], s[3]), hi = pack4<FORMAT>(s[4], s[5], s[6], s[7]);
-    uint8_t *at = q.codes + row * q.ld + blk * kBlock;
-    if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<uint32_t *>(at + 4 * l16) = lo;
-        *reinterpret_cast<uint32_t *>(at + 64 + 4 * l16) = hi;
-    } else {
-        *reinterpret_cast<uint2 *>(at + 8 * l16) = make_uint2(lo, hi);
-    }
-    if (l16 == 0) q.scales[row * q.ld_scale + blk] = (uint8_t)byte;
+    const uint32_t byte = block_scale<FORMAT>(row16_max(largest<8>(v)));
+    const float scale = scale_of(byte);
+    store_codes<T>(q, row, blk, l16, make_uint2(code4<FORMAT>(v[0], v[1], v[2], v[3], scale), code4<FORMAT>(v[4], v[5], v[6], v[7], scale)), byte);
 }
 
 }  // namespace stx
