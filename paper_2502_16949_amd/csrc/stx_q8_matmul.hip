@@ -219,12 +219,13 @@ __device__ inline void leave_sync()
 // A workgroup's outputs turn in LDS, so that its rows leave whole: as they stand, a store would have 16 bytes of 32 rows.  PASSES
 // parts of a wavefront's rows after each other, so many as NW * 8 KB need.  Pieces of 16 bytes are permuted by the row.  All
 // wavefronts call it, when nothing else of that LDS is in use; their own requests have arrived before the first store, which a
-// wait for them would wait for too.
+// wait for them would wait for too.  (LDS by instructions of its own: the compiler would wait for all requests before them.)
 template <class T, bool PAST, int BM, int BN, int WM, int WN, int MI, int NI>
-__device__ inline void leave_as(const MmArgs &p, int split, int64_t m0, int64_t n0, const f32x16_t (&acc)[MI][NI], uint8_t *lds)
+__device__ inline void leave_as(const MmArgs &p, int split, int64_t m0, int64_t n0, const f32x16_t (&acc)[MI][NI], uint32_t lds)
 {
     constexpr int PASSES = BM * BN * sizeof(T) / (WM * WN * 8192), ROWS = BM / PASSES, PART = MI / PASSES, LINE = BN * sizeof(T), PIECES = LINE / 16;
     constexpr int PER = 1024 / LINE, NW = WM * WN;           // rows of a wavefront's store
+    static_assert(ROWS == 8 * NW * PER, "eight stores of a wavefront a pass");
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));         // (no address of these is kept through the products)
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l31 = lane & 31, half = lane >> 5;
@@ -234,40 +235,50 @@ __device__ inline void leave_as(const MmArgs &p, int split, int64_t m0, int64_t 
         if (pass) leave_sync();
 #pragma unroll
         for (int i = 0; i < PART; ++i) {
-            uint8_t *line = lds + ((wm * PART + i) * 32 + l31) * LINE;
+            const uint32_t line = lds + ((wm * PART + i) * 32 + l31) * LINE;
 #pragma unroll
             for (int j = 0; j < NI; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const f32x16_t &v = acc[pass * PART + i][j];
                     const int byte = (wn + j * 32 + q * 8 + half * 4) * (int)sizeof(T);
-                    uint8_t *at = line + ((byte >> 4) ^ (l31 & 15)) * 16 + (byte & 15);
+                    const uint32_t at = line + ((byte >> 4) ^ (l31 & 15)) * 16 + (byte & 15);
                     if constexpr (sizeof(T) == 4) {
-                        *reinterpret_cast<f32x4_t *>(at) = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                        const f32x4_t four = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                        asm volatile("ds_write_b128 %0, %1" :: "v"(at), "v"(four) : "memory");
                     } else {
-                        uint32_t w[2];
+                        typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+                        u32x2_t four;
 #pragma unroll
                         for (int r = 0; r < 2; ++r)
-                            w[r] = from_float<T>(v[4 * q + 2 * r]) | (uint32_t)from_float<T>(v[4 * q + 2 * r + 1]) << 16;
-                        *reinterpret_cast<uint2 *>(at) = make_uint2(w[0], w[1]);
+                            four[r] = from_float<T>(v[4 * q + 2 * r]) | (uint32_t)from_float<T>(v[4 * q + 2 * r + 1]) << 16;
+                        asm volatile("ds_write_b64 %0, %1" :: "v"(at), "v"(four) : "memory");
                     }
                 }
         }
         if (pass == 0) __builtin_amdgcn_s_waitcnt(0x0f70);
         leave_sync();
-#pragma unroll 4
-        for (int it = 0; it < ROWS / (NW * PER); ++it) {
-            const int lr = (it * NW + wave) * PER + lane / PIECES, c = (lane % PIECES) ^ (lr & 15);
-            const i32x4_t v = *reinterpret_cast<const i32x4_t *>(lds + lr * LINE + (lane % PIECES) * 16);
+        const int r0 = wave * PER + lane / PIECES, c = lane % PIECES;           // rows r0, r0 + NW * PER, ...
+        i32x4_t v[8];
+        asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:%9\n\tds_read_b128 %2, %8 offset:%10\n\t"
+                     "ds_read_b128 %3, %8 offset:%11\n\tds_read_b128 %4, %8 offset:%12\n\tds_read_b128 %5, %8 offset:%13\n\t"
+                     "ds_read_b128 %6, %8 offset:%14\n\tds_read_b128 %7, %8 offset:%15\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+                     : "v"(lds + r0 * LINE + c * 16), "n"(NW * 1024), "n"(2 * NW * 1024), "n"(3 * NW * 1024), "n"(4 * NW * 1024),
+                       "n"(5 * NW * 1024), "n"(6 * NW * 1024), "n"(7 * NW * 1024) : "memory");
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int lr = it * NW * PER + r0, at = c ^ (lr & 15);
             const int64_t row = m0 + (lr / (PART * 32)) * (BM / WM) + pass * (PART * 32) + lr % (PART * 32);
-            if constexpr (sizeof(T) == 4) store_piece<4, PAST>((float *)p.out, p, split, row, n0 + c * 4, __builtin_bit_cast(f4u_t, v));
-            else store_piece<8, PAST>((uint16_t *)p.out, p, 0, row, n0 + c * 8, __builtin_bit_cast(u16x8u_t, v));
+            if constexpr (sizeof(T) == 4) store_piece<4, PAST>((float *)p.out, p, split, row, n0 + at * 4, __builtin_bit_cast(f4u_t, v[it]));
+            else store_piece<8, PAST>((uint16_t *)p.out, p, 0, row, n0 + at * 8, __builtin_bit_cast(u16x8u_t, v[it]));
         }
     }
 }
 template <bool WIDE, int BM, int BN, int WM, int WN, int MI, int NI>
-__device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0, const f32x16_t (&acc)[MI][NI], uint8_t *lds)
+__device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0, const f32x16_t (&acc)[MI][NI], uint32_t lds)
 {
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");       // the last products are whole (the compiler knows no reads of an asm block)
     if (WIDE || p.dtype == STX_F32) {
         if (p.past) leave_as<float, true, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
         else leave_as<float, false, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
@@ -294,7 +305,7 @@ __device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0,
 //
 // (of stage s; group 1 still multiplies s - 1 in phase 4s).  A stage's codes of A are requested beside the first reads of the stage before,
 // when everybody has read their buffer, those of B, which only one group reads, between that group's products two stages before.
-// (All of them beside the reads made those phases the longest: 8,192 x 8,192 x 8,192 in 460 us, so in 438.)  Every wavefront waits for its own
+// (All of them beside the reads made those phases the longest: 8,192 x 8,192 x 8,192 in 460 us, so in 438, with outputs as they leave now 421.)  Every wavefront waits for its own
 // at the end of 4s + 3, before the first read of the next stage; group 0 leaves those in flight that it has just requested.
 //
 // One workgroup for each compute unit takes every 256th tile, and requests the next one's first stage before its outputs leave (4,096 x
@@ -438,7 +449,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
             fetch_a(0);
             all_b(0);
         }
-        leave<WIDE, BM, BN, WM, WN>(p, split_out, m_out, n_out, acc, s_buf + BUF);
+        leave<WIDE, BM, BN, WM, WN>(p, split_out, m_out, n_out, acc, (uint32_t)(uintptr_t)(lds_ptr_t)&s_buf[BUF]);
         if (!more) break;
         phase_end();
     }
@@ -584,10 +595,11 @@ static MmPlan mm_plan(int64_t m, int64_t n, int64_t k, bool wide)
         t.ntn = (n + 16 * t.ni - 1) / (16 * t.ni);
         return t;
     }
-    // Tiles of 256 x 256 where they fill three quarters of the compute units (14,951 x 1,024 over 8,192 columns, 236 tiles, bf16: 130 us,
-    // in 128 x 128 142; 8,192 x 1,024 over 14,976, 128 tiles: 171 and 144).  Widened, where the matrix instructions take twice as long,
-    // 256 x 128 otherwise, if they do (the same sizes: 256 tiles in 193 us, in 256 x 256 259, in 128 x 128 234; without widening
-    // 151).  Below, tiles of 128 x 128, and the columns cut into slices until two workgroups for each compute unit are there.
+    // Tiles of 256 x 256 where they fill three quarters of the compute units (14,951 x 1,024 over 8,192 columns, 236 tiles, bf16: 123 us,
+    // in 128 x 128 142; 8,192 x 1,024 over 14,976, 128 tiles: 171 and 142).  Widened, where the matrix instructions take twice as long,
+    // 256 x 128 otherwise, if they do (the same sizes: 256 tiles in 191 us, in 256 x 256 260, in 128 x 128 226; without widening
+    // 151, so more than in 128 x 128).  Below, tiles of 128 x 128, and the columns cut into slices until two workgroups for each
+    // compute unit are there.
     auto tiles_of = [&](int64_t bm, int64_t bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
     t.bm = tiles_of(256, 256) >= 192 || (wide && tiles_of(256, 128) >= 192) ? 256 : 128;
     t.bn = tiles_of(256, 256) >= 192 ? 256 : 128;
