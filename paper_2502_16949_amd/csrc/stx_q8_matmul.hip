@@ -305,11 +305,11 @@ __device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0,
 //
 // (of stage s; group 1 still multiplies s - 1 in phase 4s).  A stage's codes of A are requested beside the first reads of the stage before,
 // when everybody has read their buffer, those of B, which only one group reads, between that group's products two stages before.
-// (All of them beside the reads made those phases the longest: 8,192 x 8,192 x 8,192 in 460 us, so in 438, with outputs as they leave now 421.)  Every wavefront waits for its own
+// (All of them beside the reads, from 64-bit addresses, made those phases the longest: 8,192 x 8,192 x 8,192 in 488 us, so in 449.)  Every wavefront waits for its own
 // at the end of 4s + 3, before the first read of the next stage; group 0 leaves those in flight that it has just requested.
 //
 // One workgroup for each compute unit takes every 256th tile, and requests the next one's first stage before its outputs leave (4,096 x
-// 14,951 bf16 over 1,024 columns in 85 us, with a workgroup for each tile in 91).
+// 14,951 bf16 over 1,024 columns in 91 us, with a workgroup for each tile in 98).
 template <int BM, int BN, int WM, int WN, bool WIDE, int FA, int FB>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
 {
