@@ -360,12 +360,14 @@ stx_status stx_rmsnorm_backward(stx_ctx *ctx, int32_t dtype, int64_t rows, int64
 
 /* Rows in 8 bits, with scales and rounding as stx_rmsnorm's q: q (rows x cols) the matrix, qt (cols x rows) its
  * transpose, whose blocks lie along the rows of x (the gradient's products sum over the other axis, and need it).
- * Either may be null, not both; both read x once.  rows >= 0, cols >= 0, both below 2^31.                     */
+ * Either may be null, not both; both read x once.  rows >= 0, cols >= 0, both below 2^31, and up to 2^42
+ * elements (2^38 with qt).                                                                                    */
 stx_status stx_q8_quantize(stx_ctx *ctx, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const void *x,
                            const stx_q8 *q, const stx_q8 *qt);
 
 /* out (a->rows x b->rows, `dtype`, ldo elements between rows) = A B^T over a->cols == b->cols columns (at least one), on
- * the matrix cores; sums are fp32, rounded once into out.  The formats of a and b may differ.  ld and ld_scale at most 2^24.
+ * the matrix cores; sums are fp32, rounded once into out.  The formats of a and b may differ.  ld and ld_scale at most
+ * 2^24, rows at most 2^30.
  * For an fp32 out products are whole.  For a 16-bit out the 8-bit instructions sum them in eights and cut off what lies
  * below 2^-13 of the largest of an eight: far less than the output's own rounding, unless nearly all of a sum cancels.
  * out shares no memory with the operands.  work: stx_q8_matmul_work_bytes bytes, 256-byte aligned (products of few
@@ -406,7 +408,7 @@ typedef struct {
 typedef struct {
     float *p;
     const void *g;
-    int64_t n;                /* elements, contiguous; blocks of 128 from the first on */
+    int64_t n;                /* elements, contiguous, up to 2^36 - 4096; blocks of 128 from the first on */
     stx_moments s;
     int32_t g_dtype;          /* STX_F32 / STX_BF16 / STX_F16 */
     uint32_t flags;

@@ -523,7 +523,7 @@ static bool adam_tensors_go(stx_ctx *c, const stx_adamw *h, const stx_adamw_tens
     for (; i < n && a.n < N; ++i) {
         const stx_adamw_tensor &t = tensors[i];
         const uint64_t need = ((uint64_t)t.n + kAdamTile - 1) / kAdamTile;
-        if (blocks + need > 0x7fffffffull) break;            // (the host has checked that one tensor fits)
+        if (blocks + need > (uint64_t)kMaxItems / kThreads) break;     // (the C entry has checked that one tensor fits)
         // (an empty tensor shares its first workgroup with the next one, which the search finds)
         a.t[a.n++] = {t.p, t.g, t.s.m, t.s.v, t.s.m_scale, t.s.v_scale, t.n, (uint32_t)blocks, (uint16_t)t.g_dtype, (uint16_t)t.flags};
         blocks += need;

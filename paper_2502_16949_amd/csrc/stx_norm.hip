@@ -256,13 +256,30 @@ size_t norm_bwd_work_bytes(int64_t rows, int64_t cols) { return ((size_t)bwd_blo
         else STX_NORM_GO(KERNEL, f16_t, BLOCKS);                         \
     } while (0)
 
-stx_status launch_rmsnorm(stx_ctx *c, int dtype, const NormArgs &a)
+stx_status launch_rmsnorm(stx_ctx *c, int dtype, const NormArgs &all)
 {
-    const int g = row_threads(a.cols);
-    const int64_t groups = row_block(g) / g;
-    const unsigned blocks = (unsigned)((a.rows + groups - 1) / groups);
-    ProfScope prof(c, "k_rmsnorm");
-    STX_NORM_TYPE(k_rmsnorm, blocks);
+    const int g = row_threads(all.cols);
+    const int64_t groups = row_block(g) / g, most = kMaxItems / row_block(g) * groups, e = dtype == STX_F32 ? 4 : 2;
+    NormArgs a = all;
+    auto behind = [&](void *p) { return p ? (char *)p + most * a.ld * e : nullptr; };
+    for (int64_t left = all.rows; left > 0; left -= most) {  // (one launch but for 16 million wide rows)
+        a.rows = left < most ? left : most;
+        const unsigned blocks = (unsigned)((a.rows + groups - 1) / groups);
+        {
+            ProfScope prof(c, "k_rmsnorm");
+            STX_NORM_TYPE(k_rmsnorm, blocks);
+        }
+        if (left <= most) break;
+        a.x = behind((void *)a.x);
+        a.residual = behind((void *)a.residual);
+        a.sum = behind(a.sum);
+        a.y = behind(a.y);
+        if (a.rstd) a.rstd += most;
+        if (a.q.codes) {
+            a.q.codes += most * a.q.ld;
+            a.q.scales += most * a.q.ld_scale;
+        }
+    }
     return hip_ok(hipGetLastError());
 }
 

@@ -110,8 +110,8 @@ stx_status stx_q8_quantize(stx_ctx *ctx, int32_t dtype, int64_t rows, int64_t co
     if (rows == 0 || cols == 0) return STX_OK;
     if (!x) return STX_ERR_NULL;
     if (!aligned(x, element(dtype))) return STX_ERR_BAD_ARG;
-    const int64_t cb = (cols + kBlock - 1) / kBlock;
-    if (rows > ((int64_t)1 << 35) / cb) return STX_ERR_UNSUPPORTED;        // workgroups of one launch
+    const int64_t cb = (cols + kBlock - 1) / kBlock, rb = (rows + kBlock - 1) / kBlock;
+    if (rows > ((int64_t)1 << 35) / cb || (qt && rb > kMaxItems / kThreads / cb)) return STX_ERR_UNSUPPORTED;
     return launch_q8_quantize(ctx, dtype, rows, cols, ld, x, q, qt);
 }
 
@@ -133,7 +133,7 @@ stx_status stx_q8_matmul(stx_ctx *ctx, const stx_q8 *a, const stx_q8 *b, int32_t
     if (a->rows == 0 || b->rows == 0) return STX_OK;
     for (const stx_q8 *q : {a, b})         // a tile's rows: 32-bit offsets
         if (q->ld > ((int64_t)1 << 24) || q->ld_scale > ((int64_t)1 << 24)) return STX_ERR_UNSUPPORTED;
-    if (a->rows > ((int64_t)1 << 44) / b->rows) return STX_ERR_UNSUPPORTED;                       // tiles of one launch
+    if (a->rows > ((int64_t)1 << 44) / b->rows || a->rows > ((int64_t)1 << 30) || b->rows > ((int64_t)1 << 30)) return STX_ERR_UNSUPPORTED;   // tiles of one launch
     if (!out) return STX_ERR_NULL;
     if (!aligned(out, element(dtype))) return STX_ERR_BAD_ARG;
     const size_t need = q8_matmul_work_bytes(a->rows, b->rows, a->cols);
@@ -151,7 +151,7 @@ stx_status stx_adamw_tensors(stx_ctx *ctx, const stx_adamw *h, const stx_adamw_t
     if (n_tensors > 0 && !tensors) return STX_ERR_NULL;
     for (int32_t i = 0; i < n_tensors; ++i) {
         const stx_adamw_tensor &t = tensors[i];
-        if (t.n < 0 || t.n > ((int64_t)1 << 42) || !row_dtype(t.g_dtype) || (t.flags & ~STX_ADAMW_NO_DECAY)) return STX_ERR_BAD_ARG;
+        if (t.n < 0 || t.n > ((int64_t)1 << 36) - 4096 || !row_dtype(t.g_dtype) || (t.flags & ~STX_ADAMW_NO_DECAY)) return STX_ERR_BAD_ARG;
         if (t.n == 0) continue;
         if (!t.p || !t.g) return STX_ERR_NULL;
         if (!aligned(t.p, 4) || !aligned(t.g, element(t.g_dtype))) return STX_ERR_BAD_ARG;

@@ -8,6 +8,7 @@
 namespace stx {
 
 constexpr int64_t kNormMaxCols = 16384;
+constexpr int64_t kMaxItems = ((int64_t)1 << 32) - 1;      // work items of one launch
 
 struct NormArgs {
     const void *x, *residual;

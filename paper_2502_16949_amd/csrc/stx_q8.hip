@@ -134,10 +134,15 @@ static void quantize_go(stx_ctx *c, int64_t rows, int64_t cols, int64_t ld, cons
     const int64_t cb = (cols + kBlock - 1) / kBlock, rb = (rows + kBlock - 1) / kBlock;
     const T *xt = (const T *)x;
     if (!qt) {
-        ProfScope prof(c, "k_q8_rows");
-        const dim3 grid((unsigned)((rows * cb + kThreads / 16 - 1) / (kThreads / 16)));
-        if (q->format == STX_E4M3) hipLaunchKernelGGL((k_q8_rows<T, STX_E4M3>), grid, dim3(kThreads), 0, c->stream, xt, rows, cols, ld, (int)cb, out_of(q));
-        else hipLaunchKernelGGL((k_q8_rows<T, STX_E5M2>), grid, dim3(kThreads), 0, c->stream, xt, rows, cols, ld, (int)cb, out_of(q));
+        const int64_t most = kMaxItems / kThreads * (kThreads / 16) / cb;       // rows of one launch
+        Q8Out to = out_of(q);
+        for (int64_t left = rows; left > 0; left -= most, xt += most * ld, to.codes += most * to.ld, to.scales += most * to.ld_scale) {
+            const int64_t now = left < most ? left : most;
+            ProfScope prof(c, "k_q8_rows");
+            const dim3 grid((unsigned)((now * cb + kThreads / 16 - 1) / (kThreads / 16)));
+            if (q->format == STX_E4M3) hipLaunchKernelGGL((k_q8_rows<T, STX_E4M3>), grid, dim3(kThreads), 0, c->stream, xt, now, cols, ld, (int)cb, to);
+            else hipLaunchKernelGGL((k_q8_rows<T, STX_E5M2>), grid, dim3(kThreads), 0, c->stream, xt, now, cols, ld, (int)cb, to);
+        }
         return;
     }
     ProfScope prof(c, "k_q8_turn");

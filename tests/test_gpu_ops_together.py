@@ -240,6 +240,30 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(again, near)
 
 
+def test_more_rows_than_one_launch_takes():
+    ctx = context()
+    rows, cols = (1 << 24) + 3, 1025                         # 256 threads a row
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device=G.DEV)
+    x[-5:] = torch.randn(5, cols, device=G.DEV)
+    rstd = torch.full((rows,), float("nan"), device=G.DEV)
+    B.stx_rmsnorm(ctx, x, None, None, EPS, None, None, None, rstd)
+    assert not rstd.isnan().any() and rstd[:-5].min() == rstd[:-5].max()
+    _, _, want = R.rmsnorm(x[-5:], None, None, EPS)
+    assert np.all(np.abs(R.f64(rstd[-5:]) / want - 1) <= RSTD)
+    del x, rstd
+    rows = (1 << 28) + 5                                     # 16 threads a row
+    x = torch.zeros(rows, 1, dtype=torch.bfloat16, device=G.DEV)
+    x[-9:] = torch.randn(9, 1, device=G.DEV)
+    q = B.Q8(rows, 1, 0, G.DEV)
+    q.scales.fill_(200)
+    B.stx_q8_quantize(ctx, x, q, None)
+    assert (q.scales[:-9, 0] == 127).all()
+    part = B.Q8.of(q.codes[-20:].contiguous(), q.scales[-20:].contiguous(), 1, 0)
+    R.check_q8(part, R.f64(x[-20:]))
+    del x, q
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_tensor_of_more_than_32_bits(bits):
     ctx, n = context(), (1 << 31) + 1027

@@ -91,6 +91,7 @@ def test_rmsnorm_backward_refusals(kw, status):
     (dict(qt=q8()), B.STX_ERR_BAD_ARG),                     # not the transpose's size
     (dict(qt=q8(rows=200, cols=4, ld=112)), B.STX_ERR_BAD_ARG),
     (dict(rows=1 << 30, cols=1 << 20, ld=1 << 20, q=q8(rows=1 << 30, cols=1 << 20, ld=1 << 20, ld_scale=1 << 13)), B.STX_ERR_UNSUPPORTED),
+    (dict(rows=1 << 20, cols=1 << 19, ld=1 << 19, q=None, qt=q8(rows=1 << 19, cols=1 << 20, ld=1 << 20, ld_scale=1 << 13)), B.STX_ERR_UNSUPPORTED),
 ])
 def test_quantize_refusals(kw, status):
     a = dict(ctx=context(), dtype=B.STX_F32, rows=4, cols=200, ld=200, x=P, q=q8(), qt=None)
@@ -114,6 +115,7 @@ def test_quantize_refusals(kw, status):
     (dict(a=q8(ld=(1 << 24) + 16)), B.STX_ERR_UNSUPPORTED),
     (dict(b=q8(ld_scale=(1 << 24) + 4)), B.STX_ERR_UNSUPPORTED),
     (dict(a=q8(rows=1 << 30), b=q8(rows=1 << 30), ldo=1 << 30), B.STX_ERR_UNSUPPORTED),
+    (dict(a=q8(rows=(1 << 30) + 1), b=q8(rows=1)), B.STX_ERR_UNSUPPORTED),
     (dict(a=q8(rows=40, cols=100_000, ld=100_096, ld_scale=784), b=q8(rows=40, cols=100_000, ld=100_096, ld_scale=784), ldo=40, work=None), B.STX_ERR_NULL),
     (dict(a=q8(rows=40, cols=100_000, ld=100_096, ld_scale=784), b=q8(rows=40, cols=100_000, ld=100_096, ld_scale=784), ldo=40, work_bytes=4), B.STX_ERR_WORKSPACE),
 ])
@@ -156,6 +158,7 @@ def test_adamw_hyperparameters(kw):
 @pytest.mark.parametrize("kw,bits,status", [
     (dict(n=0, p=None, g=None), 32, B.STX_OK),
     (dict(n=-1), 32, B.STX_ERR_BAD_ARG),
+    (dict(n=(1 << 36) - 4095), 32, B.STX_ERR_BAD_ARG),
     (dict(p=None), 32, B.STX_ERR_NULL),
     (dict(g=None), 32, B.STX_ERR_NULL),
     (dict(p=P + 2), 32, B.STX_ERR_BAD_ARG),
