@@ -9,7 +9,7 @@
 
 namespace stx {
 
-constexpr int kThreads = 256;          // every kernel here runs 256-thread workgroups (4 wavefronts)
+constexpr int kThreads = 256;          // threads of a workgroup (4 wavefronts), but in k_rmsnorm, its backward pass and k_q8_mm
 constexpr int kSortItems = 4;          // keys per thread in the radix-sort kernels
 constexpr int kSortTile = kThreads * kSortItems;
 constexpr int kBigSortItems = 16;      // ... in large sorts: a digit's keys of one tile then fill whole memory lines
