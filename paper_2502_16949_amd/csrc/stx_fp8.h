@@ -135,9 +135,25 @@ __device__ inline void load_octet_as(const float *row, int blk, int l16, int64_t
     }
 }
 
-// Rounds v to T and, if row is not null, stores it there.
+// A store past the caches, if `past`.  (Without something between them the compiler makes one plain store of the two.)
+#define STX_STORE_PAST(TYPE)                                       \
+    __device__ inline void store_past(TYPE v, TYPE *at, bool past) \
+    {                                                            \
+        if (past) {                                              \
+            asm volatile("");                                    \
+            __builtin_nontemporal_store(v, at);                  \
+            asm volatile("");                                    \
+        } else {                                                 \
+            *at = v;                                             \
+        }                                                        \
+    }
+STX_STORE_PAST(f4u_t)
+STX_STORE_PAST(u16x8u_t)
+#undef STX_STORE_PAST
+
+// Rounds v to T and, if row is not null, stores it there; past the caches, if `past`.
 template <class T>
-__device__ inline void round_store_octet(T *row, int blk, int l16, int64_t n, float (&v)[8])
+__device__ inline void round_store_octet(T *row, int blk, int l16, int64_t n, float (&v)[8], bool past)
 {
     if constexpr (sizeof(T) == 4) {
         if (!row) return;
@@ -146,7 +162,7 @@ __device__ inline void round_store_octet(T *row, int blk, int l16, int64_t n, fl
             const int64_t at = (int64_t)blk * kBlock + h * 64 + 4 * l16;
             if (at + 4 <= n) {
                 const f4u_t q = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-                *reinterpret_cast<f4u_t *>(row + at) = q;
+                store_past(q, reinterpret_cast<f4u_t *>(row + at), past);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -164,7 +180,7 @@ __device__ inline void round_store_octet(T *row, int blk, int l16, int64_t n, fl
         uint16_t *r16 = reinterpret_cast<uint16_t *>(row);
         const int64_t at = (int64_t)blk * kBlock + 8 * l16;
         if (at + 8 <= n) {
-            *reinterpret_cast<u16x8u_t *>(r16 + at) = q;
+            store_past(q, reinterpret_cast<u16x8u_t *>(r16 + at), past);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)

@@ -67,7 +67,7 @@ stx_status stx_rmsnorm(stx_ctx *ctx, int32_t dtype, int64_t rows, int64_t cols, 
     if (!aligned(x, e) || !aligned(residual, e) || !aligned(sum, e) || !aligned(y, e) || !aligned(weight, 4) || !aligned(rstd, 4))
         return STX_ERR_BAD_ARG;
     const NormArgs a{x, residual, weight, eps, sum, y, q ? Q8Out{q->codes, q->scales, q->ld, q->ld_scale} : Q8Out{}, q ? q->format : 0,
-                     rstd, rows, cols, ld};
+                     rstd, rows, cols, ld, false};
     return launch_rmsnorm(ctx, dtype, a);
 }
 
@@ -94,7 +94,7 @@ stx_status stx_rmsnorm_backward(stx_ctx *ctx, int32_t dtype, int64_t rows, int64
     if (need > 0 && !work) return STX_ERR_NULL;
     if (need > 0 && (work_bytes < need || !aligned(work, 256))) return STX_ERR_WORKSPACE;
     if (rows == 0 && !dweight) return STX_OK;
-    const NormBwdArgs a{sum, weight, rstd, dy, dsum, dx, dweight ? (float *)work : nullptr, rows, cols, ld};
+    const NormBwdArgs a{sum, weight, rstd, dy, dsum, dx, dweight ? (float *)work : nullptr, rows, cols, ld, false};
     return launch_rmsnorm_backward(ctx, dtype, a, dweight);
 }
 

@@ -19,6 +19,7 @@ struct NormArgs {
     int32_t format;
     float *rstd;
     int64_t rows, cols, ld;
+    bool past;                             // (set by the launcher)
 };
 struct NormBwdArgs {
     const void *sum;
@@ -27,6 +28,7 @@ struct NormBwdArgs {
     void *dx;
     float *partials;                       // [workgroups][cols], or null
     int64_t rows, cols, ld;
+    bool past;                             // (set by the launcher)
 };
 stx_status launch_rmsnorm(stx_ctx *, int dtype, const NormArgs &);
 size_t norm_bwd_work_bytes(int64_t rows, int64_t cols);

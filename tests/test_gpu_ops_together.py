@@ -156,7 +156,8 @@ def test_two_contexts_on_two_streams():
 
 # more rows than the workgroups of a backward pass take at once, for each number of threads a row
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("rows,cols", [(40_003, 100), (20_001, 250), (9_001, 500), (5_001, 700), (2_101, 2000), (1_300, 4001), (900, 8000), (700, 9001)])
+@pytest.mark.parametrize("rows,cols", [(40_003, 100), (20_001, 250), (9_001, 500), (5_001, 700), (2_101, 2000), (1_300, 4001), (900, 8000), (700, 9001),
+                                       (16_500, 1024), (33_000, 1024)])
 def test_norm_of_many_rows(rows, cols, dtype):
     ctx, rng = context(), np.random.default_rng(rows)
     x, dy, dsum = (rows_of(rng, rows, cols, dtype) for _ in range(3))
