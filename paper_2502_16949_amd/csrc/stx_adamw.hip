@@ -21,9 +21,9 @@ namespace stx {
 // Tensors of one launch: their descriptions travel as kernel arguments.  4 KB of them, or, for up to 8 tensors, 0.8 KB
 // (a call on 6 small ones takes the host 10.4 us with 4 KB, so 9.5).
 constexpr int kAdamTensors = 48, kAdamFew = 8;
-// Octets of a thread: a workgroup takes 4,096 elements (one octet: 4,000,000 x 128 in 8 bits in 1,344 us, two: 1,320).
-constexpr int kAdamOctets = 2;
-constexpr int kAdamTile = kThreads * 8 * kAdamOctets;
+// Octets of a thread: two (4,000,000 x 128 in 8 bits in 1,320 us, with one in 1,344), or one where workgroups of 4,096 elements
+// would leave compute units idle (6 tensors of 34,000 elements in 8 bits: the kernel takes 4.8 us, with two 6.2).
+constexpr int adam_tile(int octets) { return kThreads * 8 * octets; }
 
 struct AdamCoef {
     float b1, om1, b2, om2;
@@ -159,14 +159,14 @@ __device__ inline float load_grad1(const void *g, int dtype, int64_t at)
 }
 
 // A thread's octets: two quads of a block, 64 elements apart (stx_fp8.h).  Its gradients; 0 for a quad that the end cuts.
-template <class T>
-__device__ inline void load_grads(const AdamTensorArg &t, int64_t blk0, int l16, float (&g)[kAdamOctets][8])
+template <class T, int O>
+__device__ inline void load_grads(const AdamTensorArg &t, int64_t blk0, int l16, float (&g)[O][8])
 {
     typedef uint16_t u16x4u_t __attribute__((ext_vector_type(4), aligned(2)));
     using Quad = typename std::conditional<sizeof(T) == 4, f4u_t, u16x4u_t>::type;
-    Quad q[kAdamOctets][2];
+    Quad q[O][2];
 #pragma unroll
-    for (int o = 0; o < kAdamOctets; ++o)
+    for (int o = 0; o < O; ++o)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int64_t at = (blk0 + o * (kThreads / 16)) * kBlock + h * 64 + 4 * l16;
@@ -174,7 +174,7 @@ __device__ inline void load_grads(const AdamTensorArg &t, int64_t blk0, int l16,
             if (at + 4 <= t.n) q[o][h] = *reinterpret_cast<const Quad *>((const T *)t.g + at);
         }
 #pragma unroll
-    for (int o = 0; o < kAdamOctets; ++o)
+    for (int o = 0; o < O; ++o)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if constexpr (sizeof(T) == 4) g[o][j] = q[o][j / 4][j & 3];
@@ -182,7 +182,7 @@ __device__ inline void load_grads(const AdamTensorArg &t, int64_t blk0, int l16,
         }
 }
 
-template <int BITS, int N>
+template <int BITS, int N, int O>
 __global__ __launch_bounds__(kThreads) void k_adamw_tensors(AdamTensorsArgs<N> a)
 {
     // the tensor of this workgroup: the last one whose first workgroup is not behind it
@@ -195,8 +195,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw_tensors(AdamTensorsArgs<N> a
     const float decay = (t.flags & STX_ADAMW_NO_DECAY) ? 0.f : k.decay;
     const bool scale_g = a.h.gscale != nullptr;
     const int l16 = threadIdx.x & 15;
-    const int64_t blk0 = (int64_t)(blockIdx.x - t.first) * (kAdamTile / kBlock) + (threadIdx.x >> 4);
-    constexpr int O = kAdamOctets;
+    const int64_t blk0 = (int64_t)(blockIdx.x - t.first) * (adam_tile(O) / kBlock) + (threadIdx.x >> 4);
     using Raw = typename std::conditional<BITS == 32, f4u_t, uint32_t>::type;
     f4u_t pq[O][2];                        // requested first, all of them; a conversion beside a load would wait for it
     Raw mq[O][2], vq[O][2];
@@ -225,9 +224,9 @@ __global__ __launch_bounds__(kThreads) void k_adamw_tensors(AdamTensorsArgs<N> a
         }
     }
     float p[O][8], m[O][8], v[O][8], g[O][8];
-    if (t.g_dtype == STX_F32) load_grads<float>(t, blk0, l16, g);
-    else if (t.g_dtype == STX_BF16) load_grads<bf16_t>(t, blk0, l16, g);
-    else load_grads<f16_t>(t, blk0, l16, g);
+    if (t.g_dtype == STX_F32) load_grads<float, O>(t, blk0, l16, g);
+    else if (t.g_dtype == STX_BF16) load_grads<bf16_t, O>(t, blk0, l16, g);
+    else load_grads<f16_t, O>(t, blk0, l16, g);
 #pragma unroll
     for (int o = 0; o < O; ++o)
 #pragma unroll
@@ -511,7 +510,7 @@ static AdamHyper make_hyper(const stx_adamw *h)
 }
 
 // Tensors from number i on, as many as one launch takes; false: all of them empty.
-template <int N>
+template <int N, int O>
 static bool adam_tensors_go(stx_ctx *c, const stx_adamw *h, const stx_adamw_tensor *tensors, int n, int &i)
 {
     AdamTensorsArgs<N> a;
@@ -522,7 +521,7 @@ static bool adam_tensors_go(stx_ctx *c, const stx_adamw *h, const stx_adamw_tens
     uint64_t blocks = 0;
     for (; i < n && a.n < N; ++i) {
         const stx_adamw_tensor &t = tensors[i];
-        const uint64_t need = ((uint64_t)t.n + kAdamTile - 1) / kAdamTile;
+        const uint64_t need = ((uint64_t)t.n + adam_tile(O) - 1) / adam_tile(O);
         if (blocks + need > (uint64_t)kMaxItems / kThreads) break;     // (the C entry has checked that one tensor fits)
         // (an empty tensor shares its first workgroup with the next one, which the search finds)
         a.t[a.n++] = {t.p, t.g, t.s.m, t.s.v, t.s.m_scale, t.s.v_scale, t.n, (uint32_t)blocks, (uint16_t)t.g_dtype, (uint16_t)t.flags};
@@ -530,17 +529,19 @@ static bool adam_tensors_go(stx_ctx *c, const stx_adamw *h, const stx_adamw_tens
     }
     if (!blocks) return false;
     ProfScope prof(c, "k_adamw_tensors");
-    if (h->bits == 8) hipLaunchKernelGGL((k_adamw_tensors<8, N>), dim3((unsigned)blocks), dim3(kThreads), 0, c->stream, a);
-    else hipLaunchKernelGGL((k_adamw_tensors<32, N>), dim3((unsigned)blocks), dim3(kThreads), 0, c->stream, a);
+    if (h->bits == 8) hipLaunchKernelGGL((k_adamw_tensors<8, N, O>), dim3((unsigned)blocks), dim3(kThreads), 0, c->stream, a);
+    else hipLaunchKernelGGL((k_adamw_tensors<32, N, O>), dim3((unsigned)blocks), dim3(kThreads), 0, c->stream, a);
     return true;
 }
 
 stx_status launch_adamw_tensors(stx_ctx *c, const stx_adamw *h, const stx_adamw_tensor *tensors, int n)
 {
+    uint64_t full = 0;
+    for (int i = 0; i < n && full < 256; ++i) full += ((uint64_t)tensors[i].n + adam_tile(2) - 1) / adam_tile(2);
+    auto *go = n <= kAdamFew ? full < 256 ? adam_tensors_go<kAdamFew, 1> : adam_tensors_go<kAdamFew, 2>
+                             : full < 256 ? adam_tensors_go<kAdamTensors, 1> : adam_tensors_go<kAdamTensors, 2>;
     bool launched = false;
-    for (int i = 0; i < n;) {
-        if (n <= kAdamFew ? adam_tensors_go<kAdamFew>(c, h, tensors, n, i) : adam_tensors_go<kAdamTensors>(c, h, tensors, n, i)) launched = true;
-    }
+    for (int i = 0; i < n;) launched |= go(c, h, tensors, n, i);
     return launched ? hip_ok(hipGetLastError()) : STX_OK;
 }
 
