@@ -467,17 +467,25 @@ __global__ __launch_bounds__(kThreads) void k_q8_join(const float *__restrict__ 
     const int64_t quads = (n + 3) / 4, q = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (q >= m * quads) return;
     const int64_t i = q / quads, j = (q - i * quads) * 4;
+    const float *r = part + i * n + j;
     f32x4_t t = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) {
-        const float *r = part + ((int64_t)s * m + i) * n + j;
-        if (j + 4 <= n) {
-            const f4u_t v = *reinterpret_cast<const f4u_t *>(r);
-            t += f32x4_t{v[0], v[1], v[2], v[3]};
-        } else {
+    if (j + 4 <= n) {
+        auto slice = [&](int s) { return *reinterpret_cast<const f4u_t *>(r + s * m * n); };
+        auto add = [&](f4u_t v) { t += f32x4_t{v[0], v[1], v[2], v[3]}; };
+        int s = 0;
+        for (; s + 4 <= splits; s += 4) {                    // four requested together
+            const f4u_t v0 = slice(s), v1 = slice(s + 1), v2 = slice(s + 2), v3 = slice(s + 3);
+            add(v0);
+            add(v1);
+            add(v2);
+            add(v3);
+        }
+        for (; s < splits; ++s) add(slice(s));
+    } else {
+        for (int s = 0; s < splits; ++s)
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (j + u < n) t[u] += r[u];
-        }
+                if (j + u < n) t[u] += r[s * m * n + u];
     }
     store4(p, 0, i, j, t);
 }
@@ -604,16 +612,18 @@ static MmPlan mm_plan(int64_t m, int64_t n, int64_t k, bool wide)
     // Tiles of 256 x 256 where they fill three quarters of the compute units (14,951 x 1,024 over 8,192 columns, 236 tiles, bf16: 123 us,
     // in 128 x 128 142; 8,192 x 1,024 over 14,976, 128 tiles: 171 and 142).  Widened, where the matrix instructions take twice as long,
     // 256 x 128 otherwise, if they do (the same sizes: 256 tiles in 191 us, in 256 x 256 260, in 128 x 128 226; without widening
-    // 151, so more than in 128 x 128).  Below, tiles of 128 x 128, and the columns cut into slices until two workgroups for each
-    // compute unit are there.
+    // 151, so more than in 128 x 128).  Below, tiles of 128 x 128.
+    // The columns are cut into slices of four blocks at least, until there is a workgroup for each compute unit: a second one on it
+    // multiplies no faster for what joining costs (2,048 x 2,048 over 2,048 bf16, 256 tiles: 15.2 us, in two slices 24.4).  Joining takes
+    // 4 us, as long as eight blocks, so up to 15 blocks stay whole (1,024 x 1,024 over 1,024: 9.3 us, in two slices 12.8; 64 x 2,000
+    // over 2,000 fp32, 16 blocks: in four slices 11.7 us, in two 14.9).
     auto tiles_of = [&](int64_t bm, int64_t bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
     t.bm = tiles_of(256, 256) >= 192 || (wide && tiles_of(256, 128) >= 192) ? 256 : 128;
     t.bn = tiles_of(256, 256) >= 192 ? 256 : 128;
     t.ntm = (m + t.bm - 1) / t.bm;
     t.ntn = (n + t.bn - 1) / t.bn;
-    const int64_t tiles = t.ntm * t.ntn, room = t.bm == 256 ? 256 : 512;
-    int64_t splits = tiles >= room ? 1 : room / tiles;
-    const int64_t most = nkb / 8 > 0 ? nkb / 8 : 1;          // eight blocks a slice at least
+    const int64_t tiles = t.ntm * t.ntn, most = nkb >= 16 ? nkb / 4 : 1;
+    int64_t splits = tiles >= 256 ? 1 : 256 / tiles;
     if (splits > most) splits = most;
     const int64_t each = (((nkb + splits - 1) / splits) + 3) / 4 * 4;
     t.kb_split = (int)each;
