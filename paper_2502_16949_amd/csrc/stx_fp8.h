@@ -1,4 +1,4 @@
-// 8-bit floats and typed row access, shared by the kernels of the 8-bit operators (stx_norm.hip, stx_q8.hip, stx_adamw.hip).
+// 8-bit floats and typed row access, shared by stx_norm.hip, stx_q8.hip, stx_q8_matmul.hip and stx_adamw.hip.
 //
 // Work on 8-bit blocks is laid out by "octets": 16 consecutive lanes (a row of the data-parallel moves) own the 128 elements of
 // a block, 8 each, so that a block's largest magnitude is four moves inside that row.  Octets of 16-bit elements are 8
@@ -264,6 +264,7 @@ __device__ inline uint32_t block_scale(uint32_t most)
     const int e = (int)(most >> 23) - top + ((most & 0x7fffffu) > 0x600000u ? 1 : 0);   // biased by 127 like fp32's
     return most == 0u ? 127u : (uint32_t)max(e, 1);
 }
+// A scale's value; bytes are 1 to 254.
 __device__ inline float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // Four numbers as codes, nearest even; what lies above the format's largest number by less than half a step rounds to it.

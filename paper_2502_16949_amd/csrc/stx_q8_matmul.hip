@@ -51,9 +51,6 @@ __device__ inline bf16x8_t widen8(int lo, int hi, float scale)
     return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A scale's value; bytes are 1 to 254.
-__device__ inline float power(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
-
 // Four consecutive outputs of a row.
 __device__ inline void store4(const MmArgs &p, int split, int64_t i, int64_t j, const f32x4_t v)
 {
@@ -126,8 +123,8 @@ __device__ inline void multiply_step(const i32x4_t (&a)[MI][2], const uint32_t (
         // A fragment's conversions stand between the products before its own, two or three of theirs to a product (left to the compiler
         // they gather where the products end: 14,951 x 1,024 over 8,192 columns 227 us, so 223)
         bf16x8_t wb[2][NI][2], wa[2][2];
-        auto widen_a = [&](int u, int s) { wa[u & 1][s] = widen8<FA>(a[u % MI][u / MI][2 * s], a[u % MI][u / MI][2 * s + 1], power(sca[u % MI])); };
-        auto widen_b = [&](int h, int j, int s) { wb[h][j][s] = widen8<FB>(b[j][h][2 * s], b[j][h][2 * s + 1], power(scb[j])); };
+        auto widen_a = [&](int u, int s) { wa[u & 1][s] = widen8<FA>(a[u % MI][u / MI][2 * s], a[u % MI][u / MI][2 * s + 1], scale_of(sca[u % MI])); };
+        auto widen_b = [&](int h, int j, int s) { wb[h][j][s] = widen8<FB>(b[j][h][2 * s], b[j][h][2 * s + 1], scale_of(scb[j])); };
         widen_b(0, 0, 0);
         widen_a(0, 0);
 #pragma unroll
@@ -309,10 +306,11 @@ __device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0,
 //   group 0    read 1st       multiply 1st   read 2nd       multiply 2nd
 //   group 1    multiply 2nd   read 1st       multiply 1st   read 2nd
 //
-// (of stage s; group 1 still multiplies s - 1 in phase 4s).  A stage's codes of A are requested beside the first reads of the stage before,
-// when everybody has read their buffer, those of B, which only one group reads, between that group's products two stages before.
-// (All of them beside the reads, from 64-bit addresses, made those phases the longest: 8,192 x 8,192 x 8,192 in 488 us, so in 449.)  Every wavefront waits for its own
-// at the end of 4s + 3, before the first read of the next stage; group 0 leaves those in flight that it has just requested.
+// (of stage s; group 1 still multiplies s - 1 in phase 4s).  A stage's codes of A are requested beside the first reads of the stage
+// before, when everybody has read their buffer, those of B, which only one group reads, between that group's products two stages
+// before.  (All of them beside the reads, from 64-bit addresses, made those phases the longest: 8,192 x 8,192 x 8,192 in 488 us, so in
+// 449.)  Every wavefront waits for its own at the end of 4s + 3, before the first read of the next stage; group 0 leaves those in
+// flight that it has just requested.
 //
 // One workgroup for each compute unit takes every 256th tile, and requests the next one's first stage before its outputs leave (4,096 x
 // 14,951 bf16 over 1,024 columns in 91 us, with a workgroup for each tile in 98).
@@ -530,13 +528,13 @@ __global__ __launch_bounds__(kThreads) void k_q8_direct(MmArgs p)
             for (int j = 0; j < NI; ++j) {
                 qb[j][0] = *reinterpret_cast<const i32x4_t *>(rb[j] + at0);
                 qb[j][1] = *reinterpret_cast<const i32x4_t *>(rb[j] + at1);
-                bb[j] = power(sb[j][kb]);
+                bb[j] = scale_of(sb[j][kb]);
             }
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 qa[i][0] = *reinterpret_cast<const i32x4_t *>(ra[i] + at0);
                 qa[i][1] = *reinterpret_cast<const i32x4_t *>(ra[i] + at1);
-                ba[i] = power(sa[i][kb]);
+                ba[i] = scale_of(sa[i][kb]);
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
