@@ -355,9 +355,9 @@ struct Q8Out {
     int64_t ld, ld_scale;
 };
 
-// An octet's codes and, by the block's first lane, its scale.
+// An octet's codes.
 template <class T>
-__device__ inline void store_codes(const Q8Out &q, int64_t row, int blk, int l16, uint2 codes, uint32_t byte)
+__device__ inline void store_codes(const Q8Out &q, int64_t row, int blk, int l16, uint2 codes)
 {
     uint8_t *at = q.codes + row * q.ld + blk * kBlock;
     if constexpr (sizeof(T) == 4) {
@@ -366,22 +366,23 @@ __device__ inline void store_codes(const Q8Out &q, int64_t row, int blk, int l16
     } else {
         *reinterpret_cast<uint2 *>(at + 8 * l16) = codes;
     }
-    if (l16 == 0) q.scales[row * q.ld_scale + blk] = (uint8_t)byte;
 }
-// Of an octet, as it lies in memory or (with the layout of T) as floats.  All 16 lanes of the block call it; elements behind the
-// last column are 0 and get codes of 0.
+// The codes and, by the block's first lane, the scale of an octet as it lies in memory or (with the layout of T) as floats.  All 16
+// lanes of the block call it; elements behind the last column are 0 and get codes of 0.
 template <class T, int FORMAT>
 __device__ inline void store_q8_octet(const Q8Out &q, int64_t row, int blk, int l16, const Octet<T> &o)
 {
     const uint32_t byte = block_scale<FORMAT>(row16_max(largest(o)));
-    store_codes<T>(q, row, blk, l16, code8<T, FORMAT>(o, scale_of(byte)), byte);
+    store_codes<T>(q, row, blk, l16, code8<T, FORMAT>(o, scale_of(byte)));
+    if (l16 == 0) q.scales[row * q.ld_scale + blk] = (uint8_t)byte;
 }
 template <class T, int FORMAT>
 __device__ inline void store_q8_octet(const Q8Out &q, int64_t row, int blk, int l16, const float (&v)[8])
 {
     const uint32_t byte = block_scale<FORMAT>(row16_max(largest<8>(v)));
     const float scale = scale_of(byte);
-    store_codes<T>(q, row, blk, l16, make_uint2(code4<FORMAT>(v[0], v[1], v[2], v[3], scale), code4<FORMAT>(v[4], v[5], v[6], v[7], scale)), byte);
+    store_codes<T>(q, row, blk, l16, make_uint2(code4<FORMAT>(v[0], v[1], v[2], v[3], scale), code4<FORMAT>(v[4], v[5], v[6], v[7], scale)));
+    if (l16 == 0) q.scales[row * q.ld_scale + blk] = (uint8_t)byte;
 }
 
 }  // namespace stx

@@ -27,7 +27,7 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 constexpr int kTurnPitch = kBlock + 8;     // bytes of a column's codes in LDS
 // Every die takes a run of consecutive blocks (workgroups go round the dies in turn), along stripes of 8 blocks of rows, so that the
 // scales of neighbours, single bytes both ways, meet in its L2 (8,192 x 14,951 bf16 both ways in 125 us in order, so in 119; 114 with
-// the transposed codes, whole lines, past the caches).
+// the transposed codes, whole lines, past the caches; now 109).
 constexpr unsigned kDies = 8, kTurnStripe = 8;
 
 // Element j of eight octets: the largest finite magnitude (bits of an fp32), for all j, and the codes.
@@ -91,9 +91,16 @@ __global__ __launch_bounds__(kThreads) void k_q8_turn(const T *__restrict__ x, i
             for (int k = 0; k < (int)sizeof(T) * 2; ++k) o[i].w[k] = row0 + i < rows ? o[i].w[k] : 0u;
     }
     if (q.codes) {
+        uint32_t byte[8];                  // (written together, these and the other way's below: beside the codes 8,192 x 14,951 bf16 took 114 us, so 109)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (row0 + i < rows) store_q8_octet<T, FORMAT>(q, row0 + i, blk, l16, o[i]);
+            byte[i] = block_scale<FORMAT>(row16_max(largest(o[i])));
+            if (row0 + i < rows) store_codes<T>(q, row0 + i, blk, l16, code8<T, FORMAT>(o[i], scale_of(byte[i])));
+        }
+        if (l16 == 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (row0 + i < rows) q.scales[(row0 + i) * q.ld_scale + blk] = (uint8_t)byte[i];
         }
     }
     uint32_t most[8];
@@ -105,13 +112,12 @@ __global__ __launch_bounds__(kThreads) void k_q8_turn(const T *__restrict__ x, i
         if ((threadIdx.x & 48) == 0) s_most[wave][octet_pos<T>(0, l16, j)] = most[j];
     }
     __syncthreads();
+    uint32_t byte_t[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int c = octet_pos<T>(0, l16, j);
-        const uint32_t byte = block_scale<FORMAT_T>(max(max(s_most[0][c], s_most[1][c]), max(s_most[2][c], s_most[3][c])));
-        *reinterpret_cast<uint2 *>(s_codes + c * kTurnPitch + rg * 8) = column_codes<T, FORMAT_T>(o, j, scale_of(byte));
-        const int64_t col = (int64_t)blk * kBlock + c;
-        if (rg == 0 && col < cols) qt.scales[col * qt.ld_scale + row_blk] = (uint8_t)byte;
+        byte_t[j] = block_scale<FORMAT_T>(max(max(s_most[0][c], s_most[1][c]), max(s_most[2][c], s_most[3][c])));
+        *reinterpret_cast<uint2 *>(s_codes + c * kTurnPitch + rg * 8) = column_codes<T, FORMAT_T>(o, j, scale_of(byte_t[j]));
     }
     __syncthreads();
 #pragma unroll
@@ -122,6 +128,13 @@ __global__ __launch_bounds__(kThreads) void k_q8_turn(const T *__restrict__ x, i
             const uint2 a = *reinterpret_cast<const uint2 *>(s_codes + c * kTurnPitch + at);
             const uint2 b = *reinterpret_cast<const uint2 *>(s_codes + c * kTurnPitch + at + 8);
             __builtin_nontemporal_store(u32x4_t{a.x, a.y, b.x, b.y}, reinterpret_cast<u32x4_t *>(qt.codes + col * qt.ld + (int64_t)row_blk * kBlock + at));
+        }
+    }
+    if (rg == 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t col = (int64_t)blk * kBlock + octet_pos<T>(0, l16, j);
+            if (col < cols) qt.scales[col * qt.ld_scale + row_blk] = (uint8_t)byte_t[j];
         }
     }
 }
