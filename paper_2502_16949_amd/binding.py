@@ -423,29 +423,33 @@ class Q8:
 
 def _rows2d(ctx, first, *others):
     """(dtype, rows, cols, ld) of matrices of one type, shape and row stride on the context's device; others may be None."""
-    (rows, cols), stride = first.shape, first.stride()
-    assert first.get_device() == ctx.index and (stride[1] == 1 or cols == 1)
+    dtype, shape, stride, index = first.dtype, first.shape, first.stride(), ctx.index
+    rows, cols = shape
+    assert first.get_device() == index and (stride[1] == 1 or cols == 1)
     ld = stride[0] if rows > 1 else cols
     for t in others:
         if t is not None:
-            assert t.dtype is first.dtype and t.shape == first.shape and t.get_device() == ctx.index
+            assert t.dtype is dtype and t.get_device() == index and t.shape == shape
             s = t.stride()
             assert s == stride or ((s[1] == 1 or cols == 1) and (s[0] == ld or rows <= 1))
-    return DTYPES[first.dtype], rows, cols, ld
+    return DTYPES[dtype], rows, cols, ld
 
 
 def _f32dev(ctx, t, n):
-    assert t is None or (t.get_device() == ctx.index and t.dtype == torch.float32 and t.is_contiguous() and t.numel() >= n)
-    return _ptr(t)
+    if t is None:
+        return None
+    assert t.get_device() == ctx.index and t.dtype is torch.float32 and t.is_contiguous() and t.numel() >= n
+    return t.data_ptr()
 
 
 def _work(ctx, work):
     """(pointer, bytes) of the aligned part of a uint8 scratch tensor."""
     if work is None:
         return None, 0
-    assert work.get_device() == ctx.index and work.dtype == torch.uint8 and work.is_contiguous()
-    wp = (work.data_ptr() + 255) // 256 * 256
-    return wp, max(0, work.numel() - (wp - work.data_ptr()))
+    assert work.get_device() == ctx.index and work.dtype is torch.uint8 and work.is_contiguous()
+    at = work.data_ptr()
+    wp = (at + 255) // 256 * 256
+    return wp, max(0, work.numel() - (wp - at))
 
 
 def _q8(ctx, q):
