@@ -85,6 +85,11 @@ __global__ __launch_bounds__(row_block(G)) void k_rmsnorm(NormArgs a)
             if (a.weight) s[it][j] *= w[j];
         }
         if (a.q.codes) {
+            if (octet_pos<T>(blk, l16, 7) >= a.cols) {       // behind the row's end: 0 times an rstd or weight that need not be finite
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (octet_pos<T>(blk, l16, j) >= a.cols) s[it][j] = 0.f;
+            }
             if (a.format == STX_E4M3) store_q8_octet<T, STX_E4M3>(a.q, row, blk, l16, s[it]);
             else store_q8_octet<T, STX_E5M2>(a.q, row, blk, l16, s[it]);
         }

@@ -142,3 +142,23 @@ def test_no_rows(ctx):
     B.stx_rmsnorm(ctx, x, None, None, 1e-6, None, x, None, None)
     B.stx_rmsnorm_backward(ctx, x, None, torch.empty(0, device=G.DEV), x, None, x, dw, torch.empty(256, dtype=torch.uint8, device=G.DEV))
     assert not dw.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [1, 5, 100, 130, 200, 300, 700, 1001, 2000, 4001, 8001, 8300])
+def test_codes_behind_the_last_column_are_zeros(ctx, cols, dtype):
+    # whatever a row holds: NaN, infinity (rstd 0), nothing but zeros without eps (rstd infinite), a weight that is not finite
+    x = torch.randn(7, cols, device=G.DEV).to(dtype)
+    x[1, cols // 2], x[2, 0], x[3], x[4, cols - 1] = float("nan"), float("inf"), 0, float("-inf")
+    w = torch.ones(cols, device=G.DEV)
+    w[cols - 1] = float("inf")
+    for weight in (None, w):
+        for fmt in (B.STX_E4M3, B.STX_E5M2):
+            q = B.Q8(7, cols, fmt, G.DEV)
+            q.codes.fill_(0x55)
+            B.stx_rmsnorm(ctx, x, None, weight, 0.0, None, None, q, None)
+            assert not q.codes[:, cols:].any()
+            # all of a row that is NaN or 0 / 0 is NaN codes
+            bad = 0x7F if fmt == B.STX_E4M3 else 0x7C
+            for row in (1, 3):
+                assert ((q.codes[row, :cols] & 0x7F) >= bad).all()
