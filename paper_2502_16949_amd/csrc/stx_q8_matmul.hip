@@ -11,7 +11,9 @@
 //
 //   fp32 outputs: codes become bfloat16 times their power of two (v_cvt_scalef32_pk_bf16_*: exact, two codes an instruction) in
 //   front of v_mfma_f32_*_bf16, whose products are whole: 1e-7 of the result, at half the rate.  The conversions go on beside the
-//   matrix instructions (three to one of 32 x 32 x 16 make it 5 % longer).
+//   matrix instructions (three to one of 32 x 32 x 16 make it 5 % longer).  Powers of two that take codes out of bfloat16's normal
+//   numbers (beyond_reach) cannot go into them: a wavefront that has met one forms its sums anew, without powers of two in the
+//   operands (sums_far).  Watching for them takes 9 instructions a stage.
 #include "stx_device.h"
 #include "stx_ops.h"
 
@@ -43,6 +45,19 @@ __device__ inline bf16x2_t widen2(int w, float scale, bool hi)
     if constexpr (FORMAT == STX_E4M3) return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
     else return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, false);
 }
+// Whether any of the scales would take codes out of bfloat16's normal numbers: E4M3's codes but 0 are 2^-9 to 448, E5M2's 2^-16 to
+// 57344.  Distances above the least byte that does not; kReach is that of the largest.
+template <int FORMAT> constexpr uint32_t kLeast = FORMAT == STX_E4M3 ? 10 : 17;
+template <int FORMAT> constexpr uint32_t kReach = (FORMAT == STX_E4M3 ? 246 : 239) - kLeast<FORMAT>;
+template <int FORMAT, int N>
+__device__ inline void widest(const uint32_t (&bytes)[N], uint32_t &most)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = max(most, bytes[i] - kLeast<FORMAT>);
+}
+template <int FA, int FB>
+__device__ inline bool beyond_reach(uint32_t most_a, uint32_t most_b) { return __ballot(most_a > kReach<FA> || most_b > kReach<FB>) != 0; }
+
 template <int FORMAT>
 __device__ inline bf16x8_t widen8(int lo, int hi, float scale)
 {
@@ -104,6 +119,49 @@ __device__ inline f32x16_t multiply32(const i32x4_t *b, uint32_t scale_b, const 
 
 // Conversions and scalars may cross, nothing else.
 __device__ inline void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }
+
+// A wavefront's sums over blocks kb, kb + step, ... of rows from i0 of A and j0 of B, straight from memory, whatever the scales: a
+// block's sum is formed of the codes as they are, and takes its power of two as it is added.  SIZE 32 or 16: that of a product.
+template <int FA, int FB, int SIZE, int MI, int NI, class V>
+__device__ inline void sums_far(const MmArgs &p, int64_t i0, int64_t j0, int kb, int end, int step, V (&acc)[MI][NI])
+{
+    constexpr int GROUPS = 64 / SIZE, REGS = SIZE * SIZE / 64;           // lanes of a row; sums of a lane
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int in = lane % SIZE, group = lane / SIZE;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = V{};
+    for (; kb < end; kb += step) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const int64_t ra = min(i0 + i * SIZE + in, p.m - 1), rb = min(j0 + j * SIZE + in, p.n - 1);
+                V t{};
+#pragma unroll
+                for (int u = 0; u < 8 / GROUPS; ++u) {       // 16 codes a lane
+                    const int at = kb * kBlock + (u * GROUPS + group) * 16;
+                    const i32x4_t a = *reinterpret_cast<const i32x4_t *>(p.a + ra * p.lda + at), b = *reinterpret_cast<const i32x4_t *>(p.b + rb * p.ldb + at);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const bf16x8_t wa = widen8<FA>(a[2 * s], a[2 * s + 1], 1.0f), wb = widen8<FB>(b[2 * s], b[2 * s + 1], 1.0f);
+                        if constexpr (SIZE == 32) t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb, wa, t, 0, 0, 0);
+                        else t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, wa, t, 0, 0, 0);
+                    }
+                    asm volatile("" ::: "memory");           // one after the other: the registers are the hot loop's
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const int ea = p.as[ra * p.ldas + kb] - 254, eb = p.bs[rb * p.ldbs + kb];
+#pragma unroll
+                for (int r = 0; r < REGS; ++r)               // (a lane holds one row of A, and of B rows in fours)
+                    acc[i][j][r] += __builtin_ldexpf(t[r], ea + __shfl(eb, r / 4 * 4 * GROUPS + group * 4 + r % 4, SIZE));
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+}
 
 // The products of a wavefront's step: 32 codes a lane and fragment.  between(u) is called after each of 2 MI parts of them.
 template <bool WIDE, int FA, int FB, int MI, int NI, class F>
@@ -375,7 +433,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
     const uint32_t lds_scale = (uint32_t)(uintptr_t)(lds_ptr_t)&s_scale[0][0];
     const uint32_t at_sa = lds_scale + 4 * (wm + l31), at_sb = lds_scale + 4 * (BM + wn + l31);
     f32x16_t acc[MI][NI];
-    uint32_t sca[MI], scb[NI];
+    uint32_t sca[MI], scb[NI], most_a = 0, most_b = 0;
     i32x4_t a[MI][2], b[NI][2];
     uint32_t fa = 0, fb = 0;
     auto read_first = [&](int s) {
@@ -384,6 +442,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
         fb = at_b + (s & 1) * BUF;
         read_step(fa, fa ^ 32u, fb, fb ^ 32u, a, b);
         read_scales(at_sa + from, at_sb + from, sca, scb);
+        if (WIDE) {
+            widest<FA>(sca, most_a);
+            widest<FB>(scb, most_b);
+        }
     };
     auto multiply = [&](auto between) {
         __builtin_amdgcn_s_setprio(1);
@@ -443,6 +505,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
         }
         if (PHASES && group == 0) phase_end();
         __builtin_amdgcn_s_waitcnt(0x0f70);
+        if (WIDE && beyond_reach<FA, FB>(most_a, most_b)) {
+            sums_far<FA, FB, 32>(p, m0 + wm, n0 + wn, split * p.kb_split, split * p.kb_split + stages, 1, acc);
+            most_a = most_b = 0;
+        }
         phase_end();
         const int64_t m_out = m0, n_out = n0;
         const int split_out = split;
@@ -508,6 +574,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_direct(MmArgs p)
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (in) {
         const uint8_t *ra[MI], *sa[MI], *rb[NI], *sb[NI];
+        uint32_t most_a = 0, most_b = 0;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int64_t r = min((tm * MI + i) * 16 + l15, p.m - 1);
@@ -523,31 +590,33 @@ __global__ __launch_bounds__(kThreads) void k_q8_direct(MmArgs p)
         for (int kb = ks; kb < p.nkb; kb += KS) {
             const int at0 = kb * kBlock + kg * 16, at1 = at0 + 64;
             i32x4_t qa[MI][2], qb[NI][2];
-            float ba[MI], bb[NI];
+            uint32_t ba[MI], bb[NI];
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
                 qb[j][0] = *reinterpret_cast<const i32x4_t *>(rb[j] + at0);
                 qb[j][1] = *reinterpret_cast<const i32x4_t *>(rb[j] + at1);
-                bb[j] = scale_of(sb[j][kb]);
+                bb[j] = sb[j][kb];
             }
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 qa[i][0] = *reinterpret_cast<const i32x4_t *>(ra[i] + at0);
                 qa[i][1] = *reinterpret_cast<const i32x4_t *>(ra[i] + at1);
-                ba[i] = scale_of(sa[i][kb]);
+                ba[i] = sa[i][kb];
             }
+            widest<FA>(ba, most_a);
+            widest<FB>(bb, most_b);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 bf16x8_t wb[NI][2];
 #pragma unroll
                 for (int j = 0; j < NI; ++j)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) wb[j][s] = widen8<FB>(qb[j][h][2 * s], qb[j][h][2 * s + 1], bb[j]);
+                    for (int s = 0; s < 2; ++s) wb[j][s] = widen8<FB>(qb[j][h][2 * s], qb[j][h][2 * s + 1], scale_of(bb[j]));
 #pragma unroll
                 for (int i = 0; i < MI; ++i) {
                     bf16x8_t wa[2];
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) wa[s] = widen8<FA>(qa[i][h][2 * s], qa[i][h][2 * s + 1], ba[i]);
+                    for (int s = 0; s < 2; ++s) wa[s] = widen8<FA>(qa[i][h][2 * s], qa[i][h][2 * s + 1], scale_of(ba[i]));
 #pragma unroll
                     for (int j = 0; j < NI; ++j)
 #pragma unroll
@@ -555,6 +624,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_direct(MmArgs p)
                 }
             }
         }
+        if (beyond_reach<FA, FB>(most_a, most_b)) sums_far<FA, FB, 16>(p, tm * MI * 16, tn * NI * 16, ks, p.nkb, KS, acc);
     }
     if constexpr (KS > 1) {
 #pragma unroll

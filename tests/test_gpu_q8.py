@@ -199,3 +199,37 @@ def test_product_of_nothing(ctx):
         a, c = (B.Q8(r, 64, 0, G.DEV) for r in (m, n))
         B.stx_q8_matmul(ctx, a, c, torch.empty(m, n, device=G.DEV))
     del b
+
+
+# bytes of scales at both ends, of a row's blocks in turn with ordinary ones: the products of each block are ordinary
+ENDS = [(3, 300, 700), (20, 300, 700), (300, 5, 400), (16, 270_000, 260), (30, 270_000, 130), (100, 120, 900), (40, 70, 5000), (300, 700, 1300),
+        (4100, 3300, 300), (3000, 3700, 520)]
+
+
+@pytest.mark.parametrize("fa,fb", [(0, 0), (0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("m,n,k", ENDS)
+def test_product_of_scales_at_both_ends(ctx, m, n, k, fa, fb):
+    rng = np.random.default_rng(m + n + 2 * fa + fb)
+    (a, _), (b, _) = _q8_of(rng, m, k, fa), _q8_of(rng, n, k, fb)
+    nb = -(-k // 128)
+    for kb in range(nb):
+        top = (rng.integers(1, 20, m), rng.integers(235, 255, n)), (rng.integers(236, 255, m), rng.integers(1, 19, n)), None
+        if top[kb % 3]:
+            a.scales[:, kb], b.scales[:, kb] = (torch.from_numpy(t.astype(np.uint8)).to(G.DEV) for t in top[kb % 3])
+    x, y = R.q8_numbers(a), R.q8_numbers(b)
+    for dtype in (torch.float32, torch.bfloat16):
+        check_product(run(ctx, a, b, dtype, n + 1), x, y, dtype, k)
+
+
+def test_product_of_rows_near_the_largest_and_smallest_numbers(ctx):
+    # what the quantiser makes of the largest fp32 numbers and of numbers below the normal ones
+    rng = np.random.default_rng(11)
+    for m, n in ((5, 200), (70, 200)):
+        big = rng.uniform(0.5, 1, (m, 256)) * 2.0**128 * (1 - 2.0**-20) * rng.choice([-1, 1], (m, 256))
+        small = rng.uniform(0.25, 1, (n, 256)) * 2.0 ** -rng.integers(120, 135, (n, 1)) * rng.choice([-1, 1], (n, 256))
+        a, b = B.Q8(m, 256, 0, G.DEV), B.Q8(n, 256, 0, G.DEV)
+        B.stx_q8_quantize(ctx, torch.from_numpy(big.astype(np.float32)).to(G.DEV), a, None)
+        B.stx_q8_quantize(ctx, torch.from_numpy(small.astype(np.float32)).to(G.DEV), b, None)
+        assert int(a.scales[:, :2].min()) >= 246 and int(b.scales[:, :2].min()) == 1 and (a.codes & 0x7F == 0x78).any() and (b.codes & 0x7F < 8).any()
+        for dtype in (torch.float32, torch.bfloat16):
+            check_product(run(ctx, a, b, dtype), R.q8_numbers(a), R.q8_numbers(b), dtype, 256)
