@@ -78,6 +78,7 @@ class stx_q8(C.Structure):
 
 
 class stx_adamw(C.Structure):
+    held, index = (), None                     # device tensors that it points to (make_adamw), and their device
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("weight_decay", C.c_double), ("step", C.c_int64), ("step_dev", C.c_void_p), ("grad_scale", C.c_void_p),
                 ("seed", C.c_uint64), ("bits", C.c_int32)]
@@ -503,11 +504,15 @@ def stx_q8_matmul(ctx: Context, a: Q8, b: Q8, out, work=None):
 
 def make_adamw(lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, bits=32, step=1, seed=0, step_dev=None,
                grad_scale=None) -> stx_adamw:
-    """Hyperparameters; a program sets .step before every call.  step_dev (int64) and grad_scale (float32) are device tensors
-    that must stay alive while it is in use."""
-    assert step_dev is None or (step_dev.is_cuda and step_dev.dtype == torch.int64)
-    assert grad_scale is None or (grad_scale.is_cuda and grad_scale.dtype == torch.float32)
-    return stx_adamw(lr, beta1, beta2, eps, weight_decay, step, _ptr(step_dev), _ptr(grad_scale), seed, bits)
+    """Hyperparameters; a program sets .step before every call.  step_dev (int64) and grad_scale (float32) are device tensors, of
+    which the first element counts, on the device of the calls' context; the result keeps them alive."""
+    h = stx_adamw(lr, beta1, beta2, eps, weight_decay, step, _ptr(step_dev), _ptr(grad_scale), seed, bits)
+    for t, dtype in ((step_dev, torch.int64), (grad_scale, torch.float32)):
+        if t is not None:
+            assert t.is_cuda and t.dtype == dtype and t.numel() > 0 and h.index in (None, t.get_device())
+            h.index = t.get_device()
+    h.held = step_dev, grad_scale
+    return h
 
 
 class _Moments:
@@ -561,11 +566,12 @@ class AdamWState:
 
 
 def stx_adamw_tensors(ctx: Context, h: stx_adamw, tensors: AdamWTensors):
-    assert tensors.n == 0 or tensors.places == {(ctx.index, h.bits)}
+    assert (tensors.n == 0 or tensors.places == {(ctx.index, h.bits)}) and h.index in (None, ctx.index)
     _check("stx_adamw_tensors", lib().stx_adamw_tensors(ctx.handle, C.byref(h), tensors.c, tensors.n))
 
 
 def stx_adamw_step(ctx: Context, p: Params, inc: Incidence, g: Grads, h: stx_adamw, s: AdamWState):
+    assert h.index in (None, ctx.index)
     for name, m in s.held.items():
         t = getattr(p, name)
         assert t is None or (m.n == t.numel() and (m.index, m.bits) == (ctx.index, h.bits) and

@@ -1,7 +1,11 @@
 """What the entry points of the operators on rows and tensors refuse, before anything is launched: no GPU needed."""
 import ctypes as C
+import gc
+import types
+import weakref
 
 import pytest
+import torch
 
 from paper_2502_16949_amd import binding as B
 
@@ -210,3 +214,46 @@ def test_adamw_step_refusals():
     assert _step(context(), h=hyper(bits=8), s=B.stx_adamw_state(B.stx_moments(P + 2, P, P, P), m, m, m)) == B.STX_ERR_BAD_ARG
     assert _step(context(), h=hyper(bits=8), s=B.stx_adamw_state(B.stx_moments(P, P), m, m, m)) == B.STX_ERR_NULL
     assert L.stx_adamw_step(None, None, None, None, None, None) == B.STX_ERR_NULL
+
+
+class _Device:
+    """Of a device tensor, what the binding looks at."""
+
+    def __init__(self, dtype, index, n=1):
+        self.dtype, self.index, self.n, self.is_cuda = dtype, index, n, True
+
+    def numel(self):
+        return self.n
+
+    def get_device(self):
+        return self.index
+
+    def data_ptr(self):
+        return P if self.n else 0
+
+
+@pytest.mark.parametrize("name,dtype", [("step_dev", torch.int64), ("grad_scale", torch.float32)])
+def test_hyperparameters_in_device_memory(name, dtype):
+    ctx = types.SimpleNamespace(index=0, handle=None)       # (no context: the library refuses what the binding lets through)
+    none = B.AdamWTensors([])
+    for index, error in ((1, AssertionError), (0, B.StxError)):
+        h = B.make_adamw(0.1, **{name: _Device(dtype, index)})
+        with pytest.raises(error):
+            B.stx_adamw_tensors(ctx, h, none)
+        inc, grads = types.SimpleNamespace(c=B.stx_incidence()), types.SimpleNamespace(c=B.stx_grads())
+        with pytest.raises(error):
+            B.stx_adamw_step(ctx, types.SimpleNamespace(c=B.stx_params()), inc, grads, h, types.SimpleNamespace(held={}, c=B.stx_adamw_state()))
+    for bad in (_Device(torch.float64, 0), _Device(dtype, 0, 0)):      # (no element: a null pointer, so no factor at all)
+        with pytest.raises(AssertionError):
+            B.make_adamw(0.1, **{name: bad})
+    with pytest.raises(AssertionError):
+        B.make_adamw(0.1, step_dev=_Device(torch.int64, 0), grad_scale=_Device(torch.float32, 1))
+    t = _Device(dtype, 0)
+    kept = weakref.ref(t)
+    h = B.make_adamw(0.1, **{name: t})
+    del t
+    gc.collect()
+    assert kept() is not None and h.index == 0
+    del h
+    gc.collect()
+    assert kept() is None
