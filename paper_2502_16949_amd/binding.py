@@ -396,6 +396,11 @@ def stx_train_step(ctx: Context, batch, inc: Incidence, p: Params, g, lr: float,
                                                   scores.data_ptr(), loss.data_ptr()))
 
 
+def _reaches(t, width):
+    """Whether a matrix of bytes lies in memory that goes on to `width` bytes of its last row."""
+    return t.shape[0] == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= (t.shape[0] - 1) * t.stride(0) + width
+
+
 class Q8:
     """A matrix in 8 bits: `codes` (rows x cols rounded up to 128) and `scales` (rows x blocks rounded up to 4), uint8."""
 
@@ -406,7 +411,8 @@ class Q8:
 
     @classmethod
     def of(cls, codes, scales, cols, format=STX_E4M3):
-        """Around tensors that a program holds already; the codes behind the last column are 0."""
+        """Around tensors that a program holds already; the codes behind the last column are 0, and rows of scales are read in
+        words, the last one too."""
         q = cls.__new__(cls)
         q._set(codes, scales, cols, format)
         return q
@@ -414,7 +420,8 @@ class Q8:
     def _set(self, codes, scales, cols, format):
         for t in (codes, scales):
             assert t.is_cuda and t.dtype == torch.uint8 and t.dim() == 2 and t.stride(1) == 1 and t.shape[0] == codes.shape[0]
-        assert codes.shape[1] >= (cols + 127) // 128 * 128 and scales.shape[1] >= (cols + 127) // 128
+        blocks = (cols + 127) // 128
+        assert codes.shape[1] >= blocks * 128 and scales.shape[1] >= blocks and _reaches(scales, (blocks + 3) // 4 * 4)
         self.codes, self.scales, self.rows, self.cols, self.format = codes, scales, codes.shape[0], cols, format
         self.index = codes.get_device()
         assert scales.get_device() == self.index

@@ -233,3 +233,18 @@ def test_product_of_rows_near_the_largest_and_smallest_numbers(ctx):
         assert int(a.scales[:, :2].min()) >= 246 and int(b.scales[:, :2].min()) == 1 and (a.codes & 0x7F == 0x78).any() and (b.codes & 0x7F < 8).any()
         for dtype in (torch.float32, torch.bfloat16):
             check_product(run(ctx, a, b, dtype), R.q8_numbers(a), R.q8_numbers(b), dtype, 256)
+
+
+def test_rows_of_scales_end_with_a_word(ctx):
+    # five blocks: the last row's word of scales 5 to 8 has to lie in memory, however narrow the view is
+    rng = np.random.default_rng(6)
+    a, x = _q8_of(rng, 40, 600, 0)
+    b, y = _q8_of(rng, 50, 600, 0)
+    with pytest.raises(AssertionError):
+        B.Q8.of(a.codes, torch.full((40, 5), 127, dtype=torch.uint8, device=G.DEV), 600)
+    room = torch.zeros(39 * 12 + 8, dtype=torch.uint8, device=G.DEV)
+    with pytest.raises(AssertionError):
+        B.Q8.of(a.codes, room[:-1].as_strided((40, 5), (12, 1), 1), 600)
+    narrow = room.as_strided((40, 5), (12, 1))
+    narrow.copy_(a.scales[:, :5])
+    check_product(run(ctx, B.Q8.of(a.codes, narrow, 600), b, torch.float32), x, y, torch.float32, 600)
