@@ -324,7 +324,7 @@ enum { STX_E4M3 = 0, STX_E5M2 = 1 };
  * of 16 and at least cols rounded up to 128; the codes from cols up to that are 0 (every call that writes a matrix
  * writes them).  scales: 4-byte aligned, ld_scale a multiple of 4 and at least the number of blocks; bytes behind the
  * last block are never used, and not written; they belong to the matrix all the same, the last row's too.  Scale bytes
- * are 1 to 254.                                                                                              */
+ * are 1 to 254.  rows: at most 2^31 - 1; cols: at most 2^31 - 129.                                             */
 typedef struct {
     uint8_t *codes;
     uint8_t *scales;
@@ -339,8 +339,8 @@ typedef struct {
  *   s = x + residual, rounded to the rows' type;  y = s * rstd * weight,  rstd = 1 / sqrt(mean(s^2) + eps)
  * x, residual (null: none), sum and y have `dtype` and ld elements between rows; weight (null: ones) and rstd are fp32.
  * sum, y, q, rstd are outputs, each may be null (not all four): s, y rounded to the rows' type, y in 8 bits (rounded
- * once, from fp32), and what the backward pass needs.  sum may be x or residual.  rows >= 0, 1 <= cols <= 16384, ld >= cols; pointers
- * aligned to their elements only.  Arithmetic is fp32, the sum over a row in a fixed order.
+ * once, from fp32), and what the backward pass needs.  sum may be x or residual.  rows: 0 to 2^31 - 1, 1 <= cols <= 16384, ld >= cols;
+ * pointers aligned to their elements only.  Arithmetic is fp32, the sum over a row in a fixed order.
  * q (rows x cols): the scale of a block is the smallest power of two, 2^-126 at least, that brings its largest finite
  * magnitude to at most the format's largest number; 1 where there is none but 0.  Codes are rounded to nearest even;
  * NaN and, in STX_E4M3, infinities become NaN codes (in STX_E5M2 infinities stay).                             */
@@ -360,14 +360,14 @@ stx_status stx_rmsnorm_backward(stx_ctx *ctx, int32_t dtype, int64_t rows, int64
 
 /* Rows in 8 bits, with scales and rounding as stx_rmsnorm's q: q (rows x cols) the matrix, qt (cols x rows) its
  * transpose, whose blocks lie along the rows of x (the gradient's products sum over the other axis, and need it).
- * Either may be null, not both; both read x once.  rows >= 0, cols >= 0, both below 2^31, and up to 2^42
- * elements (2^38 with qt).                                                                                    */
+ * Either may be null, not both; both read x once.  rows and cols may be 0; at most 2^35 blocks of 128 columns, and with
+ * qt fewer than 2^24 blocks of 128 x 128, of which parts count whole.                                         */
 stx_status stx_q8_quantize(stx_ctx *ctx, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const void *x,
                            const stx_q8 *q, const stx_q8 *qt);
 
 /* out (a->rows x b->rows, `dtype`, ldo elements between rows) = A B^T over a->cols == b->cols columns (at least one), on
  * the matrix cores; sums are fp32, rounded once into out.  The formats of a and b may differ.  ld and ld_scale at most
- * 2^24, rows at most 2^30.
+ * 2^24, rows at most 2^30, and a->rows * b->rows at most 2^44.
  * For an fp32 out products are whole.  For a 16-bit out the 8-bit instructions sum them in eights and cut off what lies
  * below 2^-13 of the largest of an eight: far less than the output's own rounding, unless nearly all of a sum cancels.
  * out shares no memory with the operands.  work: stx_q8_matmul_work_bytes bytes, 256-byte aligned (products of few

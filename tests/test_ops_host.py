@@ -265,3 +265,28 @@ def test_memory_behind_the_last_row():
         assert B._reaches(t, width)
     for t, width in ((torch.zeros(4, 5, dtype=torch.uint8), 8), (room.view(8, 8)[:, 4:5], 8), (room[8:].view(7, 8)[6:, 6:], 4), (room.as_strided((8, 5), (8, 1), 3), 8)):
         assert not B._reaches(t, width)
+
+
+I31 = (1 << 31) - 1
+
+
+def test_limits_as_documented():
+    """The largest sizes pass their check (and meet a missing pointer), the next ones do not."""
+    ctx, x = context(), B.STX_ERR_NULL
+    quantize = lambda rows, cols, q, qt, at=None: L.stx_q8_quantize(ctx, 0, rows, cols, max(cols, 1), at, q and C.byref(q), qt and C.byref(qt))  # noqa: E731
+    of = lambda rows, cols: q8(rows, cols, ld=(cols + 127) // 128 * 128, ld_scale=((cols + 127) // 128 + 3) // 4 * 4)  # noqa: E731
+    wide = I31 - 128
+    assert quantize(1, wide, of(1, wide), None) == x and quantize(wide, 1, None, of(1, wide)) == x
+    assert quantize(1, wide + 1, of(1, wide + 1), None) == B.STX_ERR_BAD_ARG and quantize(wide + 1, 1, None, of(1, wide + 1)) == B.STX_ERR_BAD_ARG
+    assert quantize(I31, 1, of(I31, 1), None) == x and quantize(I31 + 1, 1, of(I31 + 1, 1), None) == B.STX_ERR_BAD_ARG
+    # one block of columns more than 2^35; 2^24 blocks of 128 x 128, whole ones and parts
+    assert quantize(I31, 17 * 128, of(I31, 17 * 128), None, P) == B.STX_ERR_UNSUPPORTED
+    for rows, cols in ((1 << 19, 1 << 19), ((1 << 30) + 1, 129)):
+        assert quantize(rows, cols, None, of(cols, rows), P) == B.STX_ERR_UNSUPPORTED
+    a30, b14 = of(1 << 30, 128), of(1 << 14, 128)
+    product = lambda a, b: L.stx_q8_matmul(ctx, C.byref(a), C.byref(b), 0, None, b.rows, P, 1 << 62)  # noqa: E731
+    assert product(a30, b14) == x and product(b14, a30) == x
+    assert product(a30, of((1 << 14) + 1, 128)) == B.STX_ERR_UNSUPPORTED and product(of((1 << 30) + 1, 128), b14) == B.STX_ERR_UNSUPPORTED
+    assert product(of(3, wide), of(2, wide)) == B.STX_ERR_UNSUPPORTED          # rows of more than 2^24 bytes
+    norm = lambda rows: L.stx_rmsnorm(ctx, 0, rows, 64, 64, None, None, None, 1e-6, None, P, None, None)  # noqa: E731
+    assert norm(I31) == x and norm(I31 + 1) == B.STX_ERR_BAD_ARG
