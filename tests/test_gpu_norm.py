@@ -162,3 +162,30 @@ def test_codes_behind_the_last_column_are_zeros(ctx, cols, dtype):
             bad = 0x7F if fmt == B.STX_E4M3 else 0x7C
             for row in (1, 3):
                 assert ((q.codes[row, :cols] & 0x7F) >= bad).all()
+
+
+# more rows than the workgroups take at once, so that the next row is under way while this one's gradient is stored
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(40_003, 100), (20_001, 250), (9_001, 500), (5_001, 700), (2_101, 2000), (1_300, 4001), (900, 8000), (700, 9001)])
+def test_backward_in_place_of_what_it_reads(ctx, rows, cols, dtype):
+    rng = np.random.default_rng(rows)
+    s, dy, dsum = (rows_of(rng, rows, cols, dtype) for _ in range(3))
+    w = torch.from_numpy(1 + 0.1 * rng.standard_normal(cols)).float().to(G.DEV)
+    rstd = torch.empty(rows, device=G.DEV)
+    B.stx_rmsnorm(ctx, s, None, w, 1e-6, None, None, None, rstd)
+    work = torch.empty(B.stx_rmsnorm_backward_work_bytes(ctx, rows, cols) + 256, dtype=torch.uint8, device=G.DEV)
+
+    def backward(dy, dsum, dx):
+        dw = torch.full((cols,), float("nan"), device=G.DEV)
+        B.stx_rmsnorm_backward(ctx, s, w, rstd, dy, dsum, dx, dw, work)
+        return dx, dw
+
+    want = backward(dy, dsum, torch.empty_like(dy))
+    for place in (0, 1):
+        d = [dy.clone(), dsum.clone()]
+        got = backward(*d, d[place])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    same = backward(dy, dy, torch.empty_like(dy))            # one gradient on both ways, and in its place
+    d = dy.clone()
+    got = backward(d, d, d)
+    assert torch.equal(got[0], same[0]) and torch.equal(got[1], same[1])

@@ -248,3 +248,59 @@ def test_rows_of_scales_end_with_a_word(ctx):
     narrow = room.as_strided((40, 5), (12, 1))
     narrow.copy_(a.scales[:, :5])
     check_product(run(ctx, B.Q8.of(a.codes, narrow, 600), b, torch.float32), x, y, torch.float32, 600)
+
+
+# Exact sums in every kernel: 128 x 128 in slices, 256 x 128 and 256 x 256 with an odd number of blocks and several tiles a workgroup,
+# few rows of either side; columns that are no whole block
+EXACT = [(40, 70, 5000), (700, 90, 9001), (6145, 1030, 1300), (5000, 4100, 900), (8200, 9000, 128), (4200, 8300, 385), (16, 3000, 700), (30, 600, 1500),
+         (16, 270_000, 200), (270_000, 20, 200)]
+
+
+@pytest.mark.parametrize("m,n,k", EXACT)
+def test_exact_sums_of_every_kernel(ctx, m, n, k):
+    # whole numbers of up to 3: every product of them is held whole, and every sum is below 2^24
+    rng = np.random.default_rng(m + n + k)
+    xs, ys = (torch.from_numpy(rng.integers(-3, 4, (r, k)).astype(np.float32)).to(G.DEV) for r in (m, n))
+    a, b = B.Q8(m, k, 0, G.DEV), B.Q8(n, k, 1, G.DEV)
+    B.stx_q8_quantize(ctx, xs, a, None)
+    B.stx_q8_quantize(ctx, ys, b, None)
+    want = torch.from_numpy(xs.cpu().numpy() @ ys.cpu().numpy().T)           # fp32: exact too
+    assert torch.equal(run(ctx, a, b, torch.float32).cpu(), want)
+    # products are at most 9, so none is cut off beside another (9 < 2^13): sums are whole, then rounded once
+    for dtype in (torch.bfloat16, torch.float16):
+        assert torch.equal(run(ctx, a, b, dtype).cpu(), want.to(dtype))
+        assert torch.equal(run(ctx, a, b, dtype, n + 3).cpu(), want.to(dtype))
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 3000, 300), (25, 900, 130), (60, 80, 9000), (130, 300, 700), (4096, 3600, 260), (4200, 8320, 300)])
+def test_product_fp16_out_of_every_kernel(ctx, m, n, k):
+    rng = np.random.default_rng(m + k)
+    (a, x), (b, y) = _q8_of(rng, m, k, 0), _q8_of(rng, n, k, 1)
+    for q in (a, b):
+        q.scales.sub_(9)
+    x, y = x * 2.0**-9, y * 2.0**-9
+    keep = np.unique(np.r_[:3, rng.integers(0, m, 100), m - 3:m].clip(0, m - 1))
+    # fp16 ends at 65504: sums from 65520 on round to infinities.  Else the bound of check_product
+    want, total = x[keep] @ y.T, np.abs(x[keep]) @ np.abs(y).T
+    tol = ((16 * -(-k // 128) + 16) * 2.0**-23 + 7 * 2.0**-13) * total
+    for ldo in (n, n + 5):
+        got = R.f64(run(ctx, a, b, torch.float16, ldo)[torch.from_numpy(keep).to(G.DEV)])
+        fine = np.isfinite(got)
+        assert fine.any() and np.all(np.abs(want[fine]) - tol[fine] < 65520)
+        assert np.all(np.abs(got - want)[fine] <= (tol + 2.0**-11 * np.abs(want) + 2.0**-25)[fine])
+        assert np.all(got[~fine] == np.sign(want[~fine]) * np.inf) and np.all(np.abs(want[~fine]) + tol[~fine] >= 65520)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_product_with_nan_rows_16_bit_out(ctx, dtype):
+    rng = np.random.default_rng(4)
+    for m, n in ((3, 200), (70, 90), (300, 300), (4096, 3600)):
+        a, b = _q8_of(rng, m, 256, 0)[0], _q8_of(rng, n, 256, 0)[0]
+        for q in (a, b):
+            q.scales.sub_(9)
+        a.codes[1, 200] = 0x7F
+        b.codes[n - 1, 3] = 0xFF
+        got = run(ctx, a, b, dtype)
+        bad = torch.zeros(m, n, dtype=torch.bool, device=G.DEV)
+        bad[1], bad[:, n - 1] = True, True
+        assert got[bad].isnan().all() and not got[~bad].isnan().any()        # (fp16: sums beyond 65504 are infinities)
