@@ -398,7 +398,7 @@ def stx_train_step(ctx: Context, batch, inc: Incidence, p: Params, g, lr: float,
 
 def _reaches(t, width):
     """Whether a matrix of bytes lies in memory that goes on to `width` bytes of its last row."""
-    return t.shape[0] == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= (t.shape[0] - 1) * t.stride(0) + width
+    return t.shape[0] == 0 or width == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= (t.shape[0] - 1) * t.stride(0) + width
 
 
 class Q8:

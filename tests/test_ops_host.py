@@ -261,7 +261,7 @@ def test_hyperparameters_in_device_memory(name, dtype):
 
 def test_memory_behind_the_last_row():
     room = torch.zeros(64, dtype=torch.uint8)
-    for t, width in ((room.view(8, 8)[:, :5], 8), (room.view(8, 8)[:, :1], 4), (room[:20].view(4, 5), 8), (room[3:51].view(6, 8)[:, :5], 8), (room[:0].view(0, 5), 8)):
+    for t, width in ((room.view(8, 8)[:, :5], 8), (room.view(8, 8)[:, :1], 4), (room[:20].view(4, 5), 8), (room[3:51].view(6, 8)[:, :5], 8), (room[:0].view(0, 5), 8), (torch.zeros(5, 0, dtype=torch.uint8), 0)):
         assert B._reaches(t, width)
     for t, width in ((torch.zeros(4, 5, dtype=torch.uint8), 8), (room.view(8, 8)[:, 4:5], 8), (room[8:].view(7, 8)[6:, 6:], 4), (room.as_strided((8, 5), (8, 1), 3), 8)):
         assert not B._reaches(t, width)
