@@ -12,8 +12,12 @@
 //   fp32 outputs: codes become bfloat16 times their power of two (v_cvt_scalef32_pk_bf16_*: exact, two codes an instruction) in
 //   front of v_mfma_f32_*_bf16, whose products are whole: 1e-7 of the result, at half the rate.  The conversions go on beside the
 //   matrix instructions (three to one of 32 x 32 x 16 make it 5 % longer).  Powers of two that take codes out of bfloat16's normal
-//   numbers (beyond_reach) cannot go into them: a wavefront that has met one forms its sums anew, without powers of two in the
-//   operands (sums_far).  Watching for them takes 9 instructions a stage.
+//   numbers cannot go into them: a wavefront that meets one moves a power of two from all its rows of A to those of B, for that block
+//   (balance); where there is none that suits all of them, it forms its sums anew in the end, without any in the operands (sums_far).
+//   Watching for them takes 9 instructions a stage.
+//
+// Times below are of calls in a row after 0.15 s of the same; cards differ by 6 %.  For some 10 ms after a rest the card lowers its
+// clock, and large products take up to 30 % longer; what then prefers another way than afterwards is said with both.
 #include "stx_device.h"
 #include "stx_ops.h"
 
@@ -36,7 +40,7 @@ struct MmArgs {
     void *out;                             // splits > 1: fp32 [split][m][n] instead, with ldo = n
     int64_t ldo;
     int dtype;
-    int past;                              // rows of out are whole lines
+    int past;                              // fp32 and bf16 outputs go past the caches (launch_q8_matmul); fp16 ones never do
 };
 
 template <int FORMAT>
@@ -45,18 +49,42 @@ __device__ inline bf16x2_t widen2(int w, float scale, bool hi)
     if constexpr (FORMAT == STX_E4M3) return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
     else return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, false);
 }
-// Whether any of the scales would take codes out of bfloat16's normal numbers: E4M3's codes but 0 are 2^-9 to 448, E5M2's 2^-16 to
-// 57344.  Distances above the least byte that does not; kReach is that of the largest.
-template <int FORMAT> constexpr uint32_t kLeast = FORMAT == STX_E4M3 ? 10 : 17;
-template <int FORMAT> constexpr uint32_t kReach = (FORMAT == STX_E4M3 ? 246 : 239) - kLeast<FORMAT>;
+// Scales with which every code but 0 becomes a normal bfloat16: E4M3's are 2^-9 to 448, E5M2's 2^-16 to 57344.
+template <int FORMAT> constexpr int kLeast = FORMAT == STX_E4M3 ? 10 : 17;
+template <int FORMAT> constexpr int kMost = FORMAT == STX_E4M3 ? 246 : 239;
 template <int FORMAT, int N>
-__device__ inline void widest(const uint32_t (&bytes)[N], uint32_t &most)
+__device__ inline bool in_reach(const uint32_t (&bytes)[N])
 {
+    uint32_t above = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) most = max(most, bytes[i] - kLeast<FORMAT>);
+    for (int i = 0; i < N; ++i) above = max(above, bytes[i] - kLeast<FORMAT>);
+    return above <= uint32_t(kMost<FORMAT> - kLeast<FORMAT>);
 }
-template <int FA, int FB>
-__device__ inline bool beyond_reach(uint32_t most_a, uint32_t most_b) { return __ballot(most_a > kReach<FA> || most_b > kReach<FB>) != 0; }
+// Least and largest of a wavefront's scales.
+template <int N>
+__device__ inline void range_of(const uint32_t (&bytes)[N], int &least, int &most)
+{
+    least = most = (int)bytes[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) { least = min(least, (int)bytes[i]); most = max(most, (int)bytes[i]); }
+    for (int d = 32; d >= 1; d >>= 1) { least = min(least, __shfl_xor(least, d, 64)); most = max(most, __shfl_xor(most, d, 64)); }
+}
+// The scales of a block, of which some are out of reach, with a power of two moved from A to B that brings all into it; false if there
+// is none.  The products stay what they are.
+template <int FA, int FB, int MI, int NI>
+__device__ inline bool balance(uint32_t (&a)[MI], uint32_t (&b)[NI])
+{
+    int a0, a1, b0, b1;
+    range_of(a, a0, a1);
+    range_of(b, b0, b1);
+    const int low = max(kLeast<FA> - a0, b1 - kMost<FB>), high = min(kMost<FA> - a1, b0 - kLeast<FB>), move = min(max(low, 0), high);
+    if (low > high) return false;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) a[i] += move;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) b[j] -= move;
+    return true;
+}
 
 template <int FORMAT>
 __device__ inline bf16x8_t widen8(int lo, int hi, float scale)
@@ -179,7 +207,7 @@ __device__ inline void multiply_step(const i32x4_t (&a)[MI][2], const uint32_t (
             }
     } else {
         // A fragment's conversions stand between the products before its own, two or three of theirs to a product (left to the compiler
-        // they gather where the products end: 14,951 x 1,024 over 8,192 columns 227 us, so 223)
+        // they gather where the products end: 14,951 x 1,024 over 8,192 columns takes 2 % longer)
         bf16x8_t wb[2][NI][2], wa[2][2];
         auto widen_a = [&](int u, int s) { wa[u & 1][s] = widen8<FA>(a[u % MI][u / MI][2 * s], a[u % MI][u / MI][2 * s + 1], scale_of(sca[u % MI])); };
         auto widen_b = [&](int h, int j, int s) { wb[h][j][s] = widen8<FB>(b[j][h][2 * s], b[j][h][2 * s + 1], scale_of(scb[j])); };
@@ -255,7 +283,7 @@ __device__ inline void phase_end()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// N consecutive outputs of a row.  PAST: a line that no other store completes, and nobody reads again soon.
+// N consecutive outputs of a row.  PAST: stored past the caches.
 template <int N, bool PAST, class T, class V>
 __device__ inline void store_piece(T *out, const MmArgs &p, int split, int64_t i, int64_t j, const V v)
 {
@@ -346,7 +374,7 @@ __device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0,
     } else if (p.dtype == STX_BF16) {
         if (p.past) leave_as<bf16_t, true, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
         else leave_as<bf16_t, false, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
-    } else {
+    } else {                               // (no kernel of its own for fp16 past the caches)
         leave_as<f16_t, false, BM, BN, WM, WN>(p, split, m0, n0, acc, lds);
     }
 }
@@ -366,12 +394,12 @@ __device__ inline void leave(const MmArgs &p, int split, int64_t m0, int64_t n0,
 //
 // (of stage s; group 1 still multiplies s - 1 in phase 4s).  A stage's codes of A are requested beside the first reads of the stage
 // before, when everybody has read their buffer, those of B, which only one group reads, between that group's products two stages
-// before.  (All of them beside the reads, from 64-bit addresses, made those phases the longest: 8,192 x 8,192 x 8,192 in 488 us, so in
-// 449.)  Every wavefront waits for its own at the end of 4s + 3, before the first read of the next stage; group 0 leaves those in
+// before.  (All of them beside the reads, from 64-bit addresses, made those phases the longest: 8,192 x 8,192 x 8,192 took 8 % longer.)
+// Every wavefront waits for its own at the end of 4s + 3, before the first read of the next stage; group 0 leaves those in
 // flight that it has just requested.
 //
 // One workgroup for each compute unit takes every 256th tile, and requests the next one's first stage before its outputs leave (4,096 x
-// 14,951 bf16 over 1,024 columns in 91 us, with a workgroup for each tile in 98).
+// 14,951 bf16 over 1,024 columns in 78 to 84 us, 7 % longer with a workgroup for each tile).
 template <int BM, int BN, int WM, int WN, bool WIDE, int FA, int FB>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
 {
@@ -433,7 +461,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
     const uint32_t lds_scale = (uint32_t)(uintptr_t)(lds_ptr_t)&s_scale[0][0];
     const uint32_t at_sa = lds_scale + 4 * (wm + l31), at_sb = lds_scale + 4 * (BM + wn + l31);
     f32x16_t acc[MI][NI];
-    uint32_t sca[MI], scb[NI], most_a = 0, most_b = 0;
+    uint32_t sca[MI], scb[NI];
+    bool far = false;
     i32x4_t a[MI][2], b[NI][2];
     uint32_t fa = 0, fb = 0;
     auto read_first = [&](int s) {
@@ -442,10 +471,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
         fb = at_b + (s & 1) * BUF;
         read_step(fa, fa ^ 32u, fb, fb ^ 32u, a, b);
         read_scales(at_sa + from, at_sb + from, sca, scb);
-        if (WIDE) {
-            widest<FA>(sca, most_a);
-            widest<FB>(scb, most_b);
-        }
+        if (WIDE && __ballot(!in_reach<FA>(sca) || !in_reach<FB>(scb)) && !balance<FA, FB>(sca, scb)) far = true;
     };
     auto multiply = [&](auto between) {
         __builtin_amdgcn_s_setprio(1);
@@ -505,9 +531,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_q8_mm(MmArgs p)
         }
         if (PHASES && group == 0) phase_end();
         __builtin_amdgcn_s_waitcnt(0x0f70);
-        if (WIDE && beyond_reach<FA, FB>(most_a, most_b)) {
+        if (WIDE && far) {
             sums_far<FA, FB, 32>(p, m0 + wm, n0 + wn, split * p.kb_split, split * p.kb_split + stages, 1, acc);
-            most_a = most_b = 0;
+            far = false;
         }
         phase_end();
         const int64_t m_out = m0, n_out = n0;
@@ -574,7 +600,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_direct(MmArgs p)
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     if (in) {
         const uint8_t *ra[MI], *sa[MI], *rb[NI], *sb[NI];
-        uint32_t most_a = 0, most_b = 0;
+        bool far = false;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int64_t r = min((tm * MI + i) * 16 + l15, p.m - 1);
@@ -603,8 +629,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_direct(MmArgs p)
                 qa[i][1] = *reinterpret_cast<const i32x4_t *>(ra[i] + at1);
                 ba[i] = sa[i][kb];
             }
-            widest<FA>(ba, most_a);
-            widest<FB>(bb, most_b);
+            if (__ballot(!in_reach<FA>(ba) || !in_reach<FB>(bb)) && !balance<FA, FB>(ba, bb)) far = true;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 bf16x8_t wb[NI][2];
@@ -624,7 +649,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_direct(MmArgs p)
                 }
             }
         }
-        if (beyond_reach<FA, FB>(most_a, most_b)) sums_far<FA, FB, 16>(p, tm * MI * 16, tn * NI * 16, ks, p.nkb, KS, acc);
+        if (far) sums_far<FA, FB, 16>(p, tm * MI * 16, tn * NI * 16, ks, p.nkb, KS, acc);
     }
     if constexpr (KS > 1) {
 #pragma unroll
@@ -664,8 +689,9 @@ static MmPlan mm_plan(int64_t m, int64_t n, int64_t k, bool wide)
     t.kb_split = (int)nkb;
     // Tiles of 16 x 16 for tables of up to 4,096 rows, where a workgroup for every 32 would leave compute units idle (16 rows by
     // 300 over 1,024 columns 3.0 us, in 16 x 32 3.5); 16 x 32 above (by 40,000 rows 10.6 us against 12.9).  From 2^18 rows on
-    // there are loads enough without sharing the columns, and tiles of 16 x 64 (16 by 4 M over 128 columns 146 us, in shared 16 x 32
-    // 179; by 40,000 over 1,024 13.2 against 10.6).  17 to 32 rows: 2 x 2 tiles (32 by 40,000 over 1,024 13.4 us, in 128 x 128 17.8).
+    // there are loads enough without sharing the columns, and tiles of 16 x 64 (16 by 4 M over 128 columns 127 us, in shared 16 x 32
+    // 179; by 40,000 over 1,024 13.2 against 10.6).  17 to 32 rows: 2 x 2 tiles (32 by 40,000 over 1,024 13.4 us, in 128 x 128 17.8;
+    // 33 rows, fp32, in 256 x 128 30).
     if (few <= 32) {
         const int64_t many = m < n ? n : m;
         const int across = few > 16 ? 2 : many >= ((int64_t)1 << 18) ? 4 : many > 4096 ? 2 : 1;
@@ -677,14 +703,14 @@ static MmPlan mm_plan(int64_t m, int64_t n, int64_t k, bool wide)
         t.ntn = (n + 16 * t.ni - 1) / (16 * t.ni);
         return t;
     }
-    // Tiles of 256 x 256 where they fill three quarters of the compute units (14,951 x 1,024 over 8,192 columns, 236 tiles, bf16: 123 us,
-    // in 128 x 128 142; 8,192 x 1,024 over 14,976, 128 tiles: 171 and 142).  Widened, where the matrix instructions take twice as long,
-    // 256 x 128 otherwise, if they do (the same sizes: 256 tiles in 191 us, in 256 x 256 260, in 128 x 128 226; without widening
-    // 151, so more than in 128 x 128).  Below, tiles of 128 x 128.
+    // Tiles of 256 x 256 where they fill three quarters of the compute units (14,951 x 1,024 over 8,192 columns, 236 tiles, bf16: 100 us,
+    // in 128 x 128 125; 8,192 x 1,024 over 14,976, 128 tiles: 117 and 124, after a rest 171 and 142).  Widened, where the matrix
+    // instructions take twice as long, 256 x 128 otherwise, if they do (the same sizes: 256 tiles in 198 us, in 256 x 256 203, in 128 x 128
+    // 217; after a rest 191, 260 and 226).  Below, tiles of 128 x 128.
     // The columns are cut into slices of four blocks at least, until there is a workgroup for each compute unit: a second one on it
-    // multiplies no faster for what joining costs (2,048 x 2,048 over 2,048 bf16, 256 tiles: 15.2 us, in two slices 24.4).  Joining takes
-    // 4 us, as long as eight blocks, so up to 15 blocks stay whole (1,024 x 1,024 over 1,024: 9.3 us, in two slices 12.8; 64 x 2,000
-    // over 2,000 fp32, 16 blocks: in four slices 11.7 us, in two 14.9).
+    // multiplies no faster for what joining costs (2,048 x 2,048 over 2,048 bf16, 256 tiles: 15.2 us, in two slices 26.7).  Joining takes
+    // 4 us, as long as eight blocks, so up to 15 blocks stay whole (1,024 x 1,024 over 1,024: 9.5 us, in two slices 14.9; 64 x 2,000
+    // over 2,000 fp32, 16 blocks: in four slices 12.5 us, in two 15.7).
     auto tiles_of = [&](int64_t bm, int64_t bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
     t.bm = tiles_of(256, 256) >= 192 || (wide && tiles_of(256, 128) >= 192) ? 256 : 128;
     t.bn = tiles_of(256, 256) >= 192 ? 256 : 128;
@@ -744,9 +770,10 @@ stx_status launch_q8_matmul(stx_ctx *c, const stx_q8 *a, const stx_q8 *b, int dt
     const MmPlan t = mm_plan(a->rows, b->rows, a->cols, wide);
     MmArgs p{a->codes, a->scales, b->codes, b->scales, a->ld, a->ld_scale, b->ld, b->ld_scale, a->rows, b->rows,
              (int)((a->cols + kBlock - 1) / kBlock), t.kb_split, t.splits, (int)t.ntm, (int)t.ntn, out, ldo, dtype, 0};
-    // Outputs beyond the caches go past them: 16,384 x 40,448 bf16 over 256 columns in 356 us in place of 452, over 1,024 (40,559)
-    // 748 in place of 924.  Rows that are not whole lines leave parts of lines, which meet in the caches only where tiles are short
-    // (4,096 x 14,951: over 128 columns 51 us past the caches and 43 through them; over 256, by 40,559, 520 and 560; over 512 63 and 66).
+    // Outputs beyond the caches go past them: 16,384 x 40,448 bf16 over 256 columns in 325 us in place of 423, over 1,024 (40,559)
+    // 721 in place of 890.  Rows that are not whole lines leave parts of lines, which meet in the caches only where tiles are short
+    // (4,096 x 14,951: over 128 columns 51 us past the caches and 35 through them; over 256, by 16,384 x 40,559, 523 and 550; over 512
+    // 62 and 55, after a rest 63 and 66).  fp16 outputs go through them (the first of these 404 us; leave).
     const int64_t size = dtype == STX_F32 ? 4 : 2;
     const bool lines = ldo * size % 128 == 0 && (uintptr_t)out % 128 == 0;
     p.past = t.splits == 1 && p.m * p.n * size >= ((int64_t)64 << 20) && (lines || p.nkb >= 2);

@@ -304,3 +304,23 @@ def test_product_with_nan_rows_16_bit_out(ctx, dtype):
         bad = torch.zeros(m, n, dtype=torch.bool, device=G.DEV)
         bad[1], bad[:, n - 1] = True, True
         assert got[bad].isnan().all() and not got[~bad].isnan().any()        # (fp16: sums beyond 65504 are infinities)
+
+
+@pytest.mark.parametrize("fa,fb", [(0, 0), (0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("m,n,k", ENDS)
+def test_product_of_rows_from_one_end_to_the_other(ctx, m, n, k, fa, fb):
+    # rows of one operand with scales of both ends in the same block: no power of two moved to the other operand suits them all
+    rng = np.random.default_rng(m + n + 2 * fa + fb)
+    (a, _), (b, _) = _q8_of(rng, m, k, fa), _q8_of(rng, n, k, fb)
+    nb = -(-k // 128)
+    near = 108 - {0: 18, 1: 25, 2: 32}[fa + fb]              # the largest sums: 2^(252 + near - 254), codes of 2^18 to 2^32, 128 columns
+    wide, other = (a, b) if n >= m else (b, a)
+    for kb in rng.choice(nb, -(-nb // 2), replace=False):
+        ends = np.where(rng.random(wide.rows) < 0.3, rng.integers(3, 9, wide.rows), np.where(rng.random(wide.rows) < 0.5, rng.integers(247, 253, wide.rows), 150))
+        wide.scales[:, kb] = torch.from_numpy(ends.astype(np.uint8)).to(G.DEV)
+        other.scales[:, kb] = torch.from_numpy(rng.integers(near - 4, near + 1, other.rows).astype(np.uint8)).to(G.DEV)
+    x, y = R.q8_numbers(a), R.q8_numbers(b)
+    want, total = x @ y.T, np.abs(x) @ np.abs(y).T
+    got = R.f64(run(ctx, a, b, torch.float32))
+    # as check_product, and three roundings a block to fp32's smallest step
+    assert np.all(np.abs(got - want) <= ((16 * nb + 16) * 2.0**-23 + R.U) * total + 3 * nb * 2.0**-149)
