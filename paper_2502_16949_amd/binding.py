@@ -539,7 +539,8 @@ class _Moments:
 
 class AdamWTensors:
     """The tensors of stx_adamw_tensors: (p, g, m, v[, m_scale, v_scale]) each; m and v are float32, or uint8 codes with a float32
-    scale for each 128 elements.  no_decay: positions of tensors without weight decay."""
+    scale for each 128 elements.  no_decay: positions of tensors without weight decay.  Addresses are taken here, once: a program
+    whose gradients are new tensors every step makes a new one every step, or keeps its gradients where they are."""
 
     def __init__(self, tensors, no_decay=()):
         self.keep, self.n = [], len(tensors)

@@ -467,6 +467,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw_rows(AdamRowsArgs a)
 }
 
 // TransR: the matrices of the relations that occur, as rows of kd elements (a multiple of 1,024); a wavefront takes 256 of them.
+// Bound by memory (1,345 matrices of 128 x 128: 90 us with moments in 32 bits, 617 MB, and 62 in 8, 353 MB; a part stays in the caches).
 struct AdamProjArgs {
     AdamHyper h;
     const int32_t *touched_cols, *n_touched, *first_rel_seg;
