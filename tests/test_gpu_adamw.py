@@ -261,3 +261,25 @@ def test_step_invalidates_a_stored_forward():
     with pytest.raises(B.StxError) as e:
         B.stx_backward(ctx, inc, params, grads)
     assert e.value.status == B.STX_ERR_STATE
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("model,dim,rel_dim", [("toruse", 64, 0), ("transh", 100, 0), ("transr", 32, 96)])
+def test_touched_rows_step_and_scale_from_device_memory(model, dim, rel_dim, bits):
+    outs = []
+    for device in (False, True):
+        ctx, inc, grads, params, rng = _model(model, 120, 9, dim, rel_dim, 23, 2, 7, B.STX_FLAG_BF16_PROJ if model == "transr" else 0)
+        names = [n for n in ("ent", "rel", "w", "proj") if getattr(params, n) is not None]
+        held = {n: moments(rng, getattr(params, n).shape[0], getattr(params, n)[0].numel(), bits)[0] for n in names}
+        if device:                                           # made here and dropped: the hyperparameters keep them
+            h = B.make_adamw(**H, bits=bits, step=0, seed=8, step_dev=torch.tensor([41], dtype=torch.int64, device=G.DEV),
+                             grad_scale=torch.tensor([0.25], device=G.DEV))
+        else:
+            h = B.make_adamw(**H, bits=bits, step=41, seed=8)
+            for g in (grads.rows, grads.w_rows, grads.proj):
+                if g is not None:
+                    g.mul_(0.25)                             # a power of two: the products are the same
+        B.stx_adamw_step(ctx, params, inc, grads, h, B.AdamWState(**held))
+        outs.append([getattr(params, n) for n in names] + [t for n in names for t in held[n]])
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)

@@ -324,3 +324,42 @@ def test_product_of_rows_from_one_end_to_the_other(ctx, m, n, k, fa, fb):
     got = R.f64(run(ctx, a, b, torch.float32))
     # as check_product, and three roundings a block to fp32's smallest step
     assert np.all(np.abs(got - want) <= ((16 * nb + 16) * 2.0**-23 + R.U) * total + 3 * nb * 2.0**-149)
+
+
+@pytest.mark.parametrize("dtype,itype", [(torch.bfloat16, torch.int16), (torch.float16, torch.int16)])
+def test_quantize_every_16_bit_number(ctx, dtype, itype):
+    # all of them, infinities and NaN among them: in order, so that blocks are of one size, and mixed; both ways
+    every = torch.arange(-32768, 32768, dtype=torch.int32).to(itype).view(dtype)
+    mixed = every[torch.randperm(65536, generator=torch.Generator().manual_seed(1))]
+    for v in (every, mixed):
+        x = v.view(512, 128).to(G.DEV)
+        for fmt in (0, 1):
+            q, qt = poisoned(512, 128, fmt), poisoned(128, 512, fmt)
+            B.stx_q8_quantize(ctx, x, q, qt)
+            R.check_q8(q, R.f64(x))
+            R.check_q8(qt, np.ascontiguousarray(R.f64(x).T))
+
+
+def _with_room(rows, cols, fmt):
+    """A matrix whose rows have room behind them, all of it filled."""
+    nb = -(-cols // 128)
+    codes = torch.full((rows + 1, nb * 128 + 32), 0x5A, dtype=torch.uint8, device=G.DEV)
+    scales = torch.full((rows + 1, (nb + 3) // 4 * 4 + 8), 0xA5, dtype=torch.uint8, device=G.DEV)
+    return B.Q8.of(codes[:rows], scales[:rows], cols, fmt), codes, scales, nb
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (5, 130), (130, 5), (257, 700), (40, 1030)])
+def test_room_behind_rows_stays_as_it_was(ctx, rows, cols, dtype):
+    x = torch.randn(rows, cols, device=G.DEV).to(dtype)
+    for call in ("norm", "rows", "turn", "both"):
+        q, codes, scales, nb = _with_room(rows, cols, 0)
+        qt, codes_t, scales_t, nbt = _with_room(cols, rows, 1)
+        if call == "norm":
+            B.stx_rmsnorm(ctx, x, None, None, 1e-6, None, None, q, None)
+        else:
+            B.stx_q8_quantize(ctx, x, q if call in ("rows", "both") else None, qt if call in ("turn", "both") else None)
+        for used, c, s, n, b in ((call != "turn", codes, scales, rows, nb), (call in ("turn", "both"), codes_t, scales_t, cols, nbt)):
+            n, b = (n, b) if used else (0, 0)
+            assert (c[:n, b * 128:] == 0x5A).all() and (c[n:] == 0x5A).all()
+            assert (s[:n, b:] == 0xA5).all() and (s[n:] == 0xA5).all() and not (s[:n, :b] == 0xA5).any()
